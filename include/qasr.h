@@ -429,6 +429,81 @@ qasr_status qasr_probe_copy(const void* src, void* dst, size_t bytes, void* stre
 int32_t qasr_probe_mfma_i8_outputs(void);
 qasr_status qasr_probe_mfma_i8(int32_t iters, int32_t* out, double* ops, void* stream);
 
+/* ---- Language-model operators: what scores or produces a transcript next to the encoders.  Token-major tensors
+ * (one row per token), int8 codes with a scale per token and per channel, float results.  Inference only, like everything here.
+ *
+ * Element types of float tensors.  Float pointers must be aligned to their element (else QASR_ERR_PARAM); rows may start anywhere
+ * else and be any distance apart (strides in elements, 0 => dense rows).  Unless a call says otherwise it enqueues one kernel. */
+enum { QASR_F32 = 0, QASR_F16 = 1, QASR_BF16 = 2 };
+
+/* The quantiser of Eq. 1 with a clipping range of its own for every row (the largest finite magnitude in it):
+ *   a[m] = max_k |x[m,k]| over finite x;  S[m] = a > 0 ? max(a / 127, 2^-126) : 1;  q[m,k] = Int(clip(x[m,k] / S[m], -127, 127))
+ * in single precision, each operation rounded once, ties to even, as qasr_quantize; an infinite x gives +-127, a NaN 0.
+ * x: [M, K] device of type x_type, row stride x_stride; q: [M, K] int8 device, row stride q_stride (what lies between rows is
+ * left as it was); scale: [M] float32.  M >= 0 (0: no-op), K >= 1, strides 0 or >= K, else QASR_ERR_SHAPE; an unknown type is
+ * QASR_ERR_PARAM; q and scale must overlap neither x nor each other. */
+qasr_status qasr_quantize_tokens(const void* x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride, int8_t* q,
+                                 int64_t q_stride, float* scale, void* stream);
+
+/* A linear layer on codes (Sec. 2.2: the integer matrix product on the quantised values, by linearity), scales applied to its result:
+ *   A = sum_k x[m,k] w[n,k]  (int32, exact);   y[m,n] = ((float)A x_scale[m]) w_scale[n] + (bias ? bias[n] : 0)
+ * in single precision, each operation rounded once, then rounded to y_type (to nearest, ties to even).
+ * x: [M, K] int8, w: [N, K] int8, y: [M, N] of y_type, row strides as given (0 => dense; what lies between rows of y is left as it
+ * was); x_scale: [M], w_scale, bias: [N] float32; all device.  Runs fastest where K, the strides of x and w and their
+ * addresses are multiples of 16.  M >= 0 (0: no-op), N >= 1, 1 <= K <= 131071 (the accumulator cannot overflow) and strides
+ * 0 or >= a row, else QASR_ERR_SHAPE; unknown y_type or reserved != 0: QASR_ERR_PARAM; y must not overlap any operand. */
+typedef struct {
+  int32_t M, N, K;
+  int32_t y_type;                          /* QASR_F32, QASR_F16, QASR_BF16 */
+  int64_t x_stride, w_stride, y_stride;    /* elements between rows; 0 => K, K, N */
+  int32_t reserved;                        /* 0 */
+} qasr_linear_desc;
+qasr_status qasr_linear_int8(const qasr_linear_desc* d, const int8_t* x, const float* x_scale, const int8_t* w,
+                             const float* w_scale, const float* bias, void* y, void* stream);
+
+/* qasr_quantize_tokens and qasr_linear_int8 in one call: x [M, K] of x_type, row stride d->x_stride; codes and scales live in the
+ * workspace (device, 256-byte aligned, >= qasr_linear_workspace_bytes(M, K), else QASR_ERR_WORKSPACE; it must overlap none of the
+ * tensors, and calls that may run at the same time need workspaces of their own).  The same bits as the two calls.  At most two kernels. */
+size_t qasr_linear_workspace_bytes(int32_t M, int32_t K);   /* HOST only; 0 on sizes that the call refuses */
+qasr_status qasr_linear_int8_dynamic(const qasr_linear_desc* d, const void* x, int32_t x_type, const int8_t* w,
+                                     const float* w_scale, const float* bias, void* y, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/* The linear layer with a matrix per group of rows (experts of a mixture): rows offsets[e] <= r < offsets[e+1] of y take w[e],
+ *   y[r,n] = ((float)(sum_k x[i,k] w[e,n,k]) x_scale[i]) w_scale[e,n] + (bias ? bias[e,n] : 0),   i = index ? index[r] : r
+ * d->l: M rows of y, N, K and strides as above; x: [x_rows, K] codes, x_scale: [x_rows]; offsets: [E+1] int32 and index: [M] int32
+ * or NULL, device; w: [E, N, K], expert stride w_expert_stride elements (0 => N * w_stride); w_scale, bias: [E, N].
+ * Groups may be empty; rows outside every group (before offsets[0], from offsets[E] on) are left as they were.  offsets should not
+ * decrease: they are taken as min(max(offset, 0), M), a group that ends before it starts is empty, and where decreasing
+ * offsets make groups share rows, or give the groups more rows than M together, the values of y are undefined (never an access out
+ * of range).  A row whose index is outside [0, x_rows) counts as codes of zero.  Errors as above; E < 1, E > 4096, x_rows < 1 or an expert
+ * stride smaller than a matrix is QASR_ERR_SHAPE, and so is x_rows < M without an index. */
+typedef struct {
+  qasr_linear_desc l;
+  int32_t E, x_rows;
+  int64_t w_expert_stride;
+} qasr_experts_desc;
+qasr_status qasr_experts_int8(const qasr_experts_desc* d, const int8_t* x, const float* x_scale, const int32_t* offsets,
+                              const int32_t* index, const int8_t* w, const float* w_scale, const float* bias, void* y,
+                              void* stream);
+
+/* Scores of given tokens under the distributions that rows of logits stand for.  Per row, with m = max_v x[v]:
+ *   s = sum_v e^(x[v] - m);  logprob[j] = (x[tokens[j]] - m) - ln s;  entropy = -sum_v p[v] ln p[v], p[v] = e^(x[v] - m) / s;
+ *   top_ids: the `top` ids of the largest logits, largest first, equal ones by the lower id;  top_logprob: their log probabilities
+ * sums in float32.  x: [rows, V] of x_type, row stride x_stride; tokens: [rows, n] int32, logprob: [rows, n] float32 (n == 0: neither
+ * is read, written or needed); entropy: [rows] float32 or NULL; top_ids int32, top_logprob float32: [rows, top] (top == 0:
+ * neither).  A logit of -infinity has probability 0 (log probability -infinity).  A row of nothing but -infinity has no
+ * distribution: log probabilities -infinity, entropy 0, ids in order.  A row with a NaN or +infinity: NaN everywhere, ids -1.
+ * A token below 0 (padding) scores 0, one >= V NaN.  rows >= 0 (0: no-op), V >= 1, n >= 0, 0 <= top <= min(V, QASR_MAX_TOP), stride 0 or >= V,
+ * else QASR_ERR_SHAPE.  workspace: device, 256-byte aligned, >= qasr_logprobs_workspace_bytes(rows, V, top) (may be 0: then NULL
+ * is fine), else QASR_ERR_WORKSPACE; calls that may run at the same time need workspaces of their own.  Outputs and workspace must not
+ * overlap x, tokens or each other.  At most two kernels. */
+#define QASR_MAX_TOP 64
+size_t qasr_logprobs_workspace_bytes(int64_t rows, int32_t V, int32_t top);   /* HOST only; 0 on sizes that the call refuses */
+qasr_status qasr_token_logprobs(const void* x, int32_t x_type, int64_t rows, int32_t V, int64_t x_stride, const int32_t* tokens,
+                                int32_t n, float* logprob, float* entropy, int32_t top, int32_t* top_ids, float* top_logprob,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
 /* Name of the kernel family this descriptor belongs to, and of the kernel that qasr_conv1d_int8 launches for
  * it over 16-byte aligned tensors (names as for qasr_encoder_op_kernel and _op_launch; host-only). */
 const char* qasr_conv1d_kernel_name(const qasr_conv1d_desc* d);

@@ -11,4 +11,6 @@ from .binding import (  # noqa: F401
     quantize, dequantize, IExp, Act, ACT_SIGMOID, ACT_SWISH, ACT_GLU, iexp_init, make_act, act_int8,
     softmax_int32, conv1d_int8_multi, MAX_RESIDUALS, observe_minmax, dyadic_from_scale, fold_bn_quantize,
     tuning_reload, static_workspace_bytes, probe_copy, probe_mfma_i8, probe_mfma_outputs, plan_slot_buffers,
+    quantize_tokens, linear_int8, linear_int8_dynamic, linear_workspace_bytes, experts_int8, token_logprobs,
+    logprobs_workspace_bytes, LinearDesc, ExpertsDesc, F32, F16, BF16, MAX_TOP,
 )

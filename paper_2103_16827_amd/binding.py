@@ -47,6 +47,21 @@ class _Op(ctypes.Structure):
                 ("n_more_res", _i32), ("more_res_slots", _i32 * (MAX_RESIDUALS - 1))]
 
 
+F32, F16, BF16 = 0, 1, 2
+MAX_TOP = 64
+
+
+class LinearDesc(ctypes.Structure):
+    """Mirror of qasr_linear_desc."""
+    _fields_ = [("M", _i32), ("N", _i32), ("K", _i32), ("y_type", _i32),
+                ("x_stride", _i64), ("w_stride", _i64), ("y_stride", _i64), ("reserved", _i32)]
+
+
+class ExpertsDesc(ctypes.Structure):
+    """Mirror of qasr_experts_desc."""
+    _fields_ = [("l", LinearDesc), ("E", _i32), ("x_rows", _i32), ("w_expert_stride", _i64)]
+
+
 class QasrError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -150,6 +165,22 @@ def lib():
         L.qasr_act_int8.argtypes = [ctypes.POINTER(Act), _vp, _i32, _i32, _i32, _i64, _i64, _vp, _vp]
         L.qasr_softmax_int32.restype = _i32
         L.qasr_softmax_int32.argtypes = [ctypes.POINTER(IExp), _vp, _i64, _i32, _vp, _vp]
+        L.qasr_quantize_tokens.restype = _i32
+        L.qasr_quantize_tokens.argtypes = [_vp, _i32, _i64, _i32, _i64, _vp, _i64, _vp, _vp]
+        ld, ed = ctypes.POINTER(LinearDesc), ctypes.POINTER(ExpertsDesc)
+        L.qasr_linear_int8.restype = _i32
+        L.qasr_linear_int8.argtypes = [ld, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+        L.qasr_linear_workspace_bytes.restype = ctypes.c_size_t
+        L.qasr_linear_workspace_bytes.argtypes = [_i32, _i32]
+        L.qasr_linear_int8_dynamic.restype = _i32
+        L.qasr_linear_int8_dynamic.argtypes = [ld, _vp, _i32, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+        L.qasr_experts_int8.restype = _i32
+        L.qasr_experts_int8.argtypes = [ed, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+        L.qasr_logprobs_workspace_bytes.restype = ctypes.c_size_t
+        L.qasr_logprobs_workspace_bytes.argtypes = [_i64, _i32, _i32]
+        L.qasr_token_logprobs.restype = _i32
+        L.qasr_token_logprobs.argtypes = [_vp, _i32, _i64, _i32, _i64, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, ctypes.c_size_t,
+                                          _vp]
         L.qasr_last_hip_error.restype = ctypes.c_char_p
         L.qasr_last_hip_error.argtypes = []
         L.qasr_status_string.restype = ctypes.c_char_p
@@ -336,6 +367,170 @@ def softmax_int32(e: IExp, x, y):
     rows, L = x.shape
     _check(lib().qasr_softmax_int32(ctypes.byref(e), _ptr(x), rows, L, _ptr(y), _stream()), "qasr_softmax_int32")
     return y
+
+
+# ---- language-model operators.  The library sees addresses alone, so what a tensor knows of itself is held against the
+# call here: a type, shape or stride that the call cannot mean, or another GPU than the current one, is a ValueError.
+_types = None
+
+
+def _torch_types():
+    global _types
+    if _types is None:
+        import torch
+        _types = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.int8: torch.int8,
+                  torch.int32: torch.int32, "int8": torch.int8, "int32": torch.int32, "f32": torch.float32}
+    return _types
+
+
+def _refuse(what, t, want):
+    raise ValueError(f"{what}: {want} wanted, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+
+
+def _float_type(t, what):
+    k = _torch_types().get(t.dtype)
+    if k.__class__ is not int:
+        _refuse(what, t, "float32, float16 or bfloat16")
+    return k
+
+
+def _rows(t, shape, what):
+    """The row stride of a matrix (0: dense) whose rows are contiguous."""
+    st = t.stride()
+    if tuple(t.shape) != shape or (st[1] != 1 and shape[1] > 1) or (st[0] < shape[1] and shape[0] > 1):
+        _refuse(what, t, f"a {shape} matrix of contiguous rows that do not overlap")
+    return st[0] if shape[0] > 1 else 0
+
+
+def _codes(t, shape, what):
+    if t.dtype is not _torch_types()["int8"]:
+        _refuse(what, t, "int8")
+    return _rows(t, shape, what)
+
+
+def _dense(t, kind, shape, what):
+    if t.dtype is not _torch_types()[kind] or tuple(t.shape) != shape or not t.is_contiguous():
+        _refuse(what, t, f"a dense {kind} tensor of {shape}")
+
+
+def _on_device(*tensors):
+    """The current stream, for tensors that are all on the current device."""
+    on = {t.get_device() for t in tensors if t is not None}
+    if len(on) != 1 or -1 in on:
+        raise ValueError(f"tensors on one GPU wanted, got {[str(t.device) for t in tensors if t is not None]}")
+    stream = _stream()
+    if _current_device() not in on:
+        raise ValueError(f"the tensors are on cuda:{on.pop()}, the current device is cuda:{_current_device()}")
+    return stream
+
+
+def _current_device():
+    import torch
+    return torch._C._cuda_getDevice()
+
+
+def _bytes(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def quantize_tokens(x, q, scale):
+    """qasr_quantize_tokens: float [M, K] -> int8 codes q [M, K] and float32 scale [M], one per row."""
+    M, K = x.shape
+    kind, xs, qs = _float_type(x, "x"), _rows(x, (M, K), "x"), _codes(q, (M, K), "q")
+    _dense(scale, "f32", (M,), "scale")
+    stream = _on_device(x, q, scale)
+    _check(lib().qasr_quantize_tokens(x.data_ptr(), kind, M, K, xs, q.data_ptr(), qs, scale.data_ptr(), stream),
+           "qasr_quantize_tokens")
+    return q, scale
+
+
+def _linear_desc(M, N, K, xs, w, w_scale, bias, y):
+    ws = _codes(w, (N, K), "w")
+    _dense(w_scale, "f32", (N,), "w_scale")
+    if bias is not None:
+        _dense(bias, "f32", (N,), "bias")
+    return LinearDesc(M, N, K, _float_type(y, "y"), xs, ws, _rows(y, (M, N), "y"), 0)
+
+
+def linear_int8(x, x_scale, w, w_scale, bias, y):
+    """qasr_linear_int8: codes x [M, K] and w [N, K] with scales [M] and [N] (and bias [N] or None) -> float y [M, N]."""
+    (M, K), N = x.shape, w.shape[0]
+    d = _linear_desc(M, N, K, _codes(x, (M, K), "x"), w, w_scale, bias, y)
+    _dense(x_scale, "f32", (M,), "x_scale")
+    stream = _on_device(x, x_scale, w, w_scale, bias, y)
+    _check(lib().qasr_linear_int8(ctypes.byref(d), x.data_ptr(), x_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), _ptr(bias),
+                                  y.data_ptr(), stream), "qasr_linear_int8")
+    return y
+
+
+def linear_workspace_bytes(M: int, K: int) -> int:
+    return int(lib().qasr_linear_workspace_bytes(M, K))
+
+
+def linear_int8_dynamic(x, w, w_scale, bias, y, workspace):
+    """qasr_linear_int8_dynamic: float x [M, K], quantised token by token in the workspace, through codes w [N, K] -> float y."""
+    (M, K), N = x.shape, w.shape[0]
+    kind = _float_type(x, "x")
+    d = _linear_desc(M, N, K, _rows(x, (M, K), "x"), w, w_scale, bias, y)
+    stream = _on_device(x, w, w_scale, bias, y, workspace)
+    _check(lib().qasr_linear_int8_dynamic(ctypes.byref(d), x.data_ptr(), kind, w.data_ptr(), w_scale.data_ptr(), _ptr(bias),
+                                          y.data_ptr(), _ptr(workspace), _bytes(workspace), stream), "qasr_linear_int8_dynamic")
+    return y
+
+
+def experts_int8(x, x_scale, offsets, index, w, w_scale, bias, y):
+    """qasr_experts_int8: rows offsets[e] .. offsets[e + 1] of y [M, N] through w[e] of codes w [E, N, K]; row r reads row
+    index[r] of the codes x [x_rows, K] (row r without an index).  Rows of y that the index has no entry for stay as they are."""
+    (rows, K), (E, N), M, out = x.shape, w.shape[:2], y.shape[0], y
+    if index is not None and index.shape[0] < M:
+        M = index.shape[0]
+        y = y[:M]
+    xs, st = _codes(x, (rows, K), "x"), w.stride()
+    if w.dim() != 3 or w.dtype is not _torch_types()["int8"] or w.shape[2] != K or (st[2] != 1 and K > 1) or \
+            (st[1] < K and N > 1) or (st[0] < st[1] * (N - 1) + K and E > 1):
+        _refuse("w", w, f"int8 of ({E}, {N}, {K}) with contiguous rows that do not overlap")
+    _dense(x_scale, "f32", (rows,), "x_scale")
+    _dense(w_scale, "f32", (E, N), "w_scale")
+    _dense(offsets, "int32", (E + 1,), "offsets")
+    if index is not None:
+        _dense(index, "int32", (M,), "index")
+    if bias is not None:
+        _dense(bias, "f32", (E, N), "bias")
+    d = ExpertsDesc(LinearDesc(M, N, K, _float_type(y, "y"), xs, st[1] if N > 1 else 0, _rows(y, (M, N), "y"), 0), E, rows,
+                    st[0] if E > 1 else 0)
+    stream = _on_device(x, x_scale, offsets, index, w, w_scale, bias, y)
+    _check(lib().qasr_experts_int8(ctypes.byref(d), x.data_ptr(), x_scale.data_ptr(), offsets.data_ptr(), _ptr(index),
+                                   w.data_ptr(), w_scale.data_ptr(), _ptr(bias), y.data_ptr(), stream), "qasr_experts_int8")
+    return out
+
+
+def logprobs_workspace_bytes(rows: int, V: int, top: int) -> int:
+    return int(lib().qasr_logprobs_workspace_bytes(rows, V, top))
+
+
+def token_logprobs(x, tokens=None, logprob=None, entropy=None, top_ids=None, top_logprob=None, workspace=None):
+    """qasr_token_logprobs on float logits x [rows, V]: log probabilities of int32 tokens [rows, n] into float32 logprob, the
+    entropy [rows], and the top alternatives' ids and log probabilities [rows, top].  What is not asked for is None."""
+    rows, V = x.shape
+    kind, xs = _float_type(x, "x"), _rows(x, (rows, V), "x")
+    n = tokens.shape[1] if tokens is not None else 0
+    top = top_ids.shape[1] if top_ids is not None else 0
+    if tokens is not None or logprob is not None:
+        if tokens is None or logprob is None:
+            raise ValueError("tokens and logprob go together")
+        _dense(tokens, "int32", (rows, n), "tokens")
+        _dense(logprob, "f32", (rows, n), "logprob")
+    if entropy is not None:
+        _dense(entropy, "f32", (rows,), "entropy")
+    if top_ids is not None or top_logprob is not None:
+        if top_ids is None or top_logprob is None:
+            raise ValueError("top_ids and top_logprob go together")
+        _dense(top_ids, "int32", (rows, top), "top_ids")
+        _dense(top_logprob, "f32", (rows, top), "top_logprob")
+    stream = _on_device(x, tokens, logprob, entropy, top_ids, top_logprob, workspace)
+    _check(lib().qasr_token_logprobs(x.data_ptr(), kind, rows, V, xs, _ptr(tokens), n, _ptr(logprob), _ptr(entropy), top,
+                                     _ptr(top_ids), _ptr(top_logprob), _ptr(workspace), _bytes(workspace), stream),
+           "qasr_token_logprobs")
 
 
 class Encoder:

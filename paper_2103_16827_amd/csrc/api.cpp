@@ -19,11 +19,7 @@ namespace {
 
 thread_local hipError_t g_last_hip = hipSuccess;   // detail behind the last QASR_ERR_HIP
 
-qasr_status hip_status(hipError_t e) {
-  if (e == hipSuccess) return QASR_OK;
-  g_last_hip = e;
-  return QASR_ERR_HIP;
-}
+qasr_status hip_status(hipError_t e) { return (qasr_status)qasr::status_of(e); }
 
 constexpr uint32_t kKnownFlags = QASR_FLAG_RELU | QASR_FLAG_W_PACKED;
 
@@ -161,6 +157,14 @@ size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 #define QASR_STATIC_WORKSPACE_BYTES ((size_t)32 << 20)
 
 }  // namespace
+
+namespace qasr {
+int status_of(hipError_t e) {
+  if (e == hipSuccess) return QASR_OK;
+  g_last_hip = e;
+  return QASR_ERR_HIP;
+}
+}  // namespace qasr
 
 struct qasr_encoder {
   struct Op {

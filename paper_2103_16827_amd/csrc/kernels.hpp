@@ -119,4 +119,44 @@ hipError_t launch_fold_quantize(const float* w, const float* b, const float* gam
                                 const float* var, float eps, int32_t Cout, int64_t per, float S_x, float S_y, int8_t* qw,
                                 int32_t* bias_q, int32_t* m, int32_t* s, float* S_w, int32_t* bad_count, hipStream_t st);
 
+// The qasr_status of a HIP call's result; remembers an error for qasr_last_hip_error (api.cpp).
+int status_of(hipError_t e);
+
+// ---- language-model operators (tokens.hip, linear.hip, logprobs.hip); types are the ABI's QASR_F32, _F16, _BF16
+hipError_t launch_quantize_tokens(const void* x, int x_type, int64_t M, int K, int64_t x_stride, int8_t* q, int64_t q_stride,
+                                  float* scale, hipStream_t st);
+
+// One linear layer, or one per group of rows (offsets != null).
+struct LinearParams {
+  const int8_t* x;
+  const float* x_scale;
+  const int8_t* w;
+  const float* w_scale;
+  const float* bias;      // may be null
+  void* y;
+  int64_t xs, ws, ys;     // elements between rows
+  int32_t M, N, K;
+  int32_t y_type;
+  // groups
+  const int32_t* offsets; // [E + 1], or null: one matrix for all rows
+  const int32_t* index;   // row of x of each row of y, or null
+  int32_t E, x_rows;
+  int64_t wes;            // elements between matrices
+};
+hipError_t launch_linear(const LinearParams& p, hipStream_t st);
+
+// One call of qasr_token_logprobs.
+struct LogprobParams {
+  const void* x;
+  const int32_t* tokens;
+  float* logprob;
+  float* entropy;         // may be null
+  int32_t* top_ids;
+  float* top_logprob;
+  int64_t rows, xs;
+  int32_t V, n, top;
+};
+size_t logprobs_workspace_bytes(int64_t rows, int V, int top);
+hipError_t launch_logprobs(const LogprobParams& p, int x_type, void* workspace, hipStream_t st);
+
 }  // namespace qasr

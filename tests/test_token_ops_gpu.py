@@ -1,0 +1,515 @@
+"""Language-model operators against their definitions in 64 bits, at the sizes and values where they can go wrong.
+
+The linear layers' results are defined bit for bit (an exact integer sum, then single-precision operations that each round
+once): equality.  Sums of exponentials are not: their tolerance counts the roundings, see _score_bounds."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2103_16827_amd as Q
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+FILL = 77
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def codes(g, *shape):
+    return torch.randint(-128, 128, shape, generator=g, dtype=torch.int32).to(torch.int8)
+
+
+def scales(g, *shape):
+    return torch.rand(*shape, generator=g) * 0.02 + 0.001
+
+
+class Padded:
+    """A matrix on the GPU whose rows are `stride` apart and whose buffer begins `shift` elements into its allocation; every
+    byte around it keeps its value."""
+
+    def __init__(self, rows, cols, dtype, stride=0, shift=0, host=None):
+        self.rows, self.cols, self.stride, self.shift = rows, cols, stride or cols, shift
+        n = shift + max(0, rows - 1) * self.stride + cols + 64
+        self.raw = torch.full((n,), FILL, dtype=dtype, device="cuda")
+        self.view = self.raw.as_strided((rows, cols), (self.stride, 1), shift)
+        if host is not None:
+            self.view.copy_(host)
+
+    def check(self):
+        rest = self.raw.clone()
+        rest.as_strided((self.rows, self.cols), (self.stride, 1), self.shift).fill_(FILL)
+        assert bool((rest == FILL).all()), "written outside the rows"
+
+
+def quantize_ref(x):
+    """(codes, scales) of the definition, in numpy's float32 (each operation rounded once)."""
+    x = x.float().numpy()
+    mag = np.where(np.isfinite(x), np.abs(x), np.float32(0))
+    a = mag.max(axis=1).astype(np.float32)
+    S = np.where(a > 0, np.maximum(a / np.float32(127), np.float32(2.0 ** -126)), np.float32(1)).astype(np.float32)
+    with np.errstate(invalid="ignore", over="ignore"):
+        t = (x / S[:, None]).astype(np.float32)
+    q = np.rint(np.clip(t, -127, 127))
+    return torch.from_numpy(np.where(np.isnan(t), 0, q).astype(np.int8)), torch.from_numpy(S)
+
+
+def linear_ref(x, xs, w, ws, bias, dtype):
+    """The definition: exact sums (in 64 bits), single-precision operations after them."""
+    acc = (x.double() @ w.double().t()).float()
+    y = acc * xs[:, None] * ws
+    if bias is not None:
+        y = y + bias
+    return y.to(dtype)
+
+
+def same(got, want, what):
+    got, want = got.cpu(), want
+    eq = (got == want) | (got.isnan() & want.isnan())
+    assert bool(eq.all()), f"{what}: {int((~eq).sum())} of {eq.numel()} values differ, first at {tuple(eq.logical_not().nonzero()[0].tolist())}"
+
+
+# ---- quantiser
+
+QROWS = [(1, 1), (3, 7), (5, 64), (2, 255), (9, 256), (4, 1000), (3, 4096), (2, 5001), (2, 16384), (1, 20011), (300, 72), (1, 70000)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,K", QROWS)
+def test_quantize_tokens(M, K, dtype):
+    print(f"[case] quantize {M} x {K} {dtype}", flush=True)
+    g = gen(M * 131 + K)
+    for pad, qpad, shift in ((0, 0, 0), (8, 16, 16), (3, 5, 1)):
+        x = (torch.randn(M, K, generator=g) * torch.rand(M, 1, generator=g) * 10).to(dtype)
+        xp, qp = Padded(M, K, dtype, K + pad, shift, x), Padded(M, K, torch.int8, K + qpad, shift)
+        scale = torch.empty(M, device="cuda")
+        Q.quantize_tokens(xp.view, qp.view, scale)
+        q, S = quantize_ref(x)
+        same(scale, S, "scales")
+        same(qp.view, q, "codes")
+        qp.check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_quantize_tokens_values(dtype):
+    """Zeros, infinities, NaN, the type's extremes, subnormals, ties."""
+    print(f"[case] quantize values {dtype}", flush=True)
+    inf, nan, fi = float("inf"), float("nan"), torch.finfo(dtype)
+    K = 40
+    x = torch.zeros(12, K, dtype=dtype)
+    x[1, 3] = -0.0
+    x[2, :4] = torch.tensor([inf, -inf, nan, 0.0])
+    x[3, :5] = torch.tensor([inf, 2.0, -1.0, nan, -inf])
+    x[4, :3] = torch.tensor([fi.max, fi.min, fi.max / 2])
+    x[5, :3] = torch.tensor([fi.smallest_normal, -fi.smallest_normal / 2, 0.0])
+    x[6, :2] = torch.tensor([fi.smallest_normal * fi.eps, -fi.smallest_normal * fi.eps])     # the smallest of all
+    x[7] = torch.arange(K).to(dtype) - 20 + 0.5
+    x[7, 0] = 127.0                                                        # scale 1: halves, ties to even
+    x[8] = nan
+    x[9] = inf
+    x[10, K - 1] = 3.0
+    x[11] = -5.0
+    q, S = quantize_ref(x)
+    qd, sd = torch.empty(12, K, dtype=torch.int8, device="cuda"), torch.empty(12, device="cuda")
+    Q.quantize_tokens(x.cuda(), qd, sd)
+    same(sd, S, "scales")
+    same(qd, q, "codes")
+
+
+# ---- linear layers
+
+SHAPES = [(1, 1, 1), (1, 16, 64), (1, 17, 65), (2, 3, 15), (3, 128, 128), (7, 129, 127), (15, 64, 16), (16, 16, 17), (17, 33, 200), (16, 512, 1024),
+          (31, 100, 320), (32, 256, 4096), (33, 65, 1008), (48, 1000, 512), (64, 64, 64), (65, 31, 96), (100, 260, 333), (127, 255, 640),
+          (128, 128, 256), (129, 384, 520), (200, 257, 1000), (256, 256, 256), (257, 513, 129), (300, 1029, 1003), (512, 768, 192),
+          (1000, 300, 80), (1025, 272, 2000), (5, 4099, 48), (2048, 16, 32)]
+
+
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_linear(M, N, K):
+    g = gen(M * 7 + N * 3 + K)
+    x, w = codes(g, M, K), codes(g, N, K)
+    xs, ws, b = scales(g, M), scales(g, N), torch.randn(N, generator=g) * 20
+    for i, (dtype, bias, pads) in enumerate([(torch.float32, None, (0, 0, 0, 0)), (torch.bfloat16, b, (16, 48, 8, 16)), (torch.float16, None, (5, 3, 1, 1)),
+                                             (torch.float32, b, (7, 0, 0, 3)), (torch.bfloat16, None, (0, 0, 3, 0))]):
+        print(f"[case] linear {M} x {N} x {K} {dtype} pads {pads}", flush=True)
+        px, pw, py, shift = pads
+        xp = Padded(M, K, torch.int8, K + px, shift, x)
+        wp = Padded(N, K, torch.int8, K + pw, shift, w)
+        yp = Padded(M, N, dtype, N + py, shift)
+        Q.linear_int8(xp.view, xs.cuda(), wp.view, ws.cuda(), None if bias is None else bias.cuda(), yp.view)
+        same(yp.view, linear_ref(x, xs, w, ws, bias, dtype), f"linear {dtype} {pads}")
+        yp.check()
+
+
+@pytest.mark.parametrize("M,N,K", [(2, 17, 131071), (40, 16, 131056), (300, 256, 131056), (300, 300, 131071)])
+def test_linear_longest_sums(M, N, K):
+    """Every product 128 x 128: the largest sums the accumulator is promised to hold, of either sign."""
+    print(f"[case] linear longest sums {M} x {N} x {K}", flush=True)
+    x = torch.full((M, K), -128, dtype=torch.int8, device="cuda")
+    w = torch.full((N, K), -128, dtype=torch.int8, device="cuda")
+    w[N // 2:] = 127
+    one = torch.ones(max(M, N), device="cuda")
+    y = torch.empty(M, N, device="cuda")
+    Q.linear_int8(x, one[:M], w, one[:N], None, y)
+    want = torch.full((M, N), float(np.float32(K * 16384)))
+    want[:, N // 2:] = float(np.float32(-K * 128 * 127))
+    same(y, want, "sums")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_scales_that_are_not_ordinary(dtype):
+    """Zero, negative, infinite and NaN scales and biases go through the three operations as they are."""
+    print(f"[case] linear scales {dtype}", flush=True)
+    g = gen(5)
+    x, w = codes(g, 20, 64), codes(g, 40, 64)
+    x[3] = 0
+    xs, ws, b = scales(g, 20), scales(g, 40), torch.randn(40, generator=g)
+    xs[0], xs[1], xs[2], xs[3] = 0.0, -1.0, float("inf"), float("inf")
+    ws[0], ws[1], ws[2], ws[3] = 0.0, -2.0, float("inf"), float("nan")
+    b[5], b[6] = float("inf"), float("nan")
+    y = torch.empty(20, 40, dtype=dtype, device="cuda")
+    Q.linear_int8(x.cuda(), xs.cuda(), w.cuda(), ws.cuda(), b.cuda(), y)
+    same(y, linear_ref(x, xs, w, ws, b, dtype), "linear")
+
+
+def test_linear_beyond_32_bits():
+    """Rows whose offsets pass 2^32 bytes, in x, w and y."""
+    print("[case] linear, offsets beyond 32 bits", flush=True)
+    g = gen(6)
+    M, N, K, far = 40, 48, 96, (1 << 27) + 32
+    big = torch.full((far * 47 + K + 64,), FILL, dtype=torch.int8, device="cuda")
+    x, w, xs, ws = codes(g, M, K), codes(g, N, K), scales(g, M), scales(g, N)
+    wv = big.as_strided((N, K), (far, 1), 0)
+    xv = big.as_strided((M, K), (far, 1), 4096)
+    wv.copy_(w)
+    xv.copy_(x)
+    y = torch.full((M, far // 2), 1.0, dtype=torch.bfloat16, device="cuda")
+    Q.linear_int8(xv, xs.cuda(), wv, ws.cuda(), None, y[:, :N])
+    same(y[:, :N], linear_ref(x, xs, w, ws, None, torch.bfloat16), "linear")
+    assert bool((y[:, N:N + 4096] == 1).all()) and bool((y[:, -4096:] == 1).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(1, 64, 64), (1, 2048, 2048), (1, 5, 3), (4, 300, 1003), (16, 128, 8192), (17, 77, 512), (33, 1000, 130), (300, 256, 384)])
+def test_linear_dynamic(M, N, K, dtype):
+    print(f"[case] dynamic linear {M} x {N} x {K} {dtype}", flush=True)
+    g = gen(M + N + K)
+    x = (torch.randn(M, K, generator=g) * 3).to(dtype)
+    x[M // 2, K // 2] = float("inf")
+    w, ws, b = codes(g, N, K), scales(g, N), torch.randn(N, generator=g)
+    q, S = quantize_ref(x)
+    for ydt, bias, pad, shift in ((torch.float32, b, 0, 0), (torch.bfloat16, None, 8, 8), (torch.float16, b, 5, 1)):
+        xp, wp, yp = Padded(M, K, dtype, K + pad, shift, x), Padded(N, K, torch.int8, K + pad, shift, w), Padded(M, N, ydt, N + pad, shift)
+        work = torch.full((Q.linear_workspace_bytes(M, K) + 256,), FILL, dtype=torch.int8, device="cuda")
+        Q.linear_int8_dynamic(xp.view, wp.view, ws.cuda(), None if bias is None else bias.cuda(), yp.view, work[:-256])
+        same(yp.view, linear_ref(q, S, w, ws, bias, ydt), f"dynamic {ydt}")
+        yp.check()
+        assert bool((work[-256:] == FILL).all())
+
+
+# ---- experts
+
+def experts_ref(x, xs, offsets, index, w, ws, bias, y):
+    y = y.clone()
+    for e in range(w.shape[0]):
+        lo, hi = offsets[e], offsets[e + 1]
+        if hi > lo:
+            i = torch.arange(lo, hi) if index is None else index[lo:hi].long()
+            y[lo:hi] = linear_ref(x[i], xs[i], w[e], ws[e], None if bias is None else bias[e], y.dtype)
+    return y
+
+
+GROUPS = [([4], 1, 16, 64), ([0, 0, 3, 0], 4, 20, 48), ([1, 2, 3, 4, 5], 16, 33, 100), ([16, 0, 17, 1], 34, 128, 256), ([0, 0, 0], 3, 64, 64),
+          ([100, 3, 0, 129], 232, 130, 333), ([300, 256, 1], 600, 256, 128), ([128] * 5, 640, 512, 1024), ([1] * 70, 80, 96, 512),
+          ([0] * 100 + [5] + [0] * 40 + [70], 75, 48, 80), ([513, 0, 31, 200], 800, 257, 520)]
+
+
+@pytest.mark.parametrize("case", range(len(GROUPS)))
+def test_experts(case):
+    sizes, M, N, K = GROUPS[case]
+    E, g = len(sizes), gen(case)
+    M = max(M, sum(sizes))
+    for j, (dtype, with_index, with_bias, first, pad) in enumerate([(torch.float32, True, True, 0, 0), (torch.bfloat16, False, False, 0, 16),
+                                                                     (torch.float16, True, False, 2, 3)]):
+        print(f"[case] experts {sizes[:8]}.. N={N} K={K} {dtype} index={with_index} first={first} pad={pad}", flush=True)
+        rows = M + first + 3
+        T = 11 if with_index else rows
+        offsets = np.concatenate([[0], np.cumsum(sizes)]) + first
+        x, xs, w, ws = codes(g, T, K), scales(g, T), codes(g, E, N, K), scales(g, E, N)
+        bias = torch.randn(E, N, generator=g) if with_bias else None
+        index = torch.randint(0, T, (rows,), generator=g).int() if with_index else None
+        xp = Padded(T, K, torch.int8, K + pad, pad, x)
+        wraw = torch.full((E * (N * (K + pad) + pad) + 64,), FILL, dtype=torch.int8, device="cuda")
+        wv = wraw.as_strided((E, N, K), (N * (K + pad) + pad, K + pad, 1), pad)
+        wv.copy_(w)
+        yp = Padded(rows, N, dtype, N + pad, 0)
+        want = experts_ref(x, xs, offsets.tolist(), index, w, ws, bias, yp.view.cpu())
+        Q.experts_int8(xp.view, xs.cuda(), torch.from_numpy(offsets.astype(np.int32)).cuda(), None if index is None else index.cuda(), wv,
+                       ws.cuda(), None if bias is None else bias.cuda(), yp.view)
+        same(yp.view, want, "experts")                 # (rows outside the groups keep FILL)
+        yp.check()
+
+
+def test_experts_offsets_and_indexes_out_of_range():
+    """Offsets below 0 and beyond M are cut off, decreasing ones are empty groups, unknown rows count as zeros."""
+    print("[case] experts, offsets and indexes out of range", flush=True)
+    g = gen(9)
+    M, N, K, T = 50, 40, 64, 10
+    x, xs, w, ws, bias = codes(g, T, K), scales(g, T), codes(g, 4, N, K), scales(g, 4, N), torch.randn(4, N, generator=g)
+    index = torch.randint(0, T, (M,), generator=g).int()
+    index[3], index[30], index[49] = -1, T, (1 << 31) - 1
+    for offsets, as_if in (([-5, 10, 10, 60, 40], [0, 10, 10, 50, 50]), ([-(1 << 31), 0, 20, 45, (1 << 31) - 1], [0, 0, 20, 45, 50]),
+                           ([7, 2, 9, 9, 30], [7, 7, 9, 9, 30])):
+        y = torch.full((M, N), float(FILL))
+        xz, xsz = torch.cat([x, torch.zeros(1, K, dtype=torch.int8)]), torch.cat([xs, torch.ones(1)])
+        idx = torch.where((index < 0) | (index >= T), torch.tensor(T, dtype=torch.int32), index)
+        want = experts_ref(xz, xsz, as_if, idx, w, ws, bias, y)
+        if offsets[0] == 7:                            # the second group begins at row 2
+            want = experts_ref(xz, xsz, [7, 7, 7, 9, 30], idx, w, ws, bias, y)
+            want[2:9] = linear_ref(xz[idx[2:9].long()], xsz[idx[2:9].long()], w[1], ws[1], bias[1], torch.float32)
+            want[9:30] = linear_ref(xz[idx[9:30].long()], xsz[idx[9:30].long()], w[3], ws[3], bias[3], torch.float32)
+        yd = y.cuda()
+        Q.experts_int8(x.cuda(), xs.cuda(), torch.tensor(offsets, dtype=torch.int64).to(torch.int32).cuda(), index.cuda(), w.cuda(), ws.cuda(),
+                       bias.cuda(), yd)
+        same(yd, want, f"offsets {offsets}")
+
+
+# ---- scores
+
+def _score_bounds(x64, m, ls, p, V):
+    """How far float32 results may be from 64 bits.  A row's sum is made of at most V/64 + 64 additions one after the other (at
+    least 64 lanes share it), each rounding by 2^-24 of a partial sum that is at most the whole; an exponential of
+    d = x - m carries 2^-24 |d| for the difference, as much again for its product with log2 e, and 2 ulp = 2^-22 of its own (the
+    hardware's exponential is 1 ulp off, its argument's rounding near 0 at most as much).  So ln s is off by at most
+    u (2 E|d| + V/64 + 68), u = 2^-24 (+ 2 ulp of the logarithm itself), the log probability by that and two differences, and
+    the entropy by twice that times 1 + E|d| (numerator, denominator)."""
+    u = 2.0 ** -24
+    with np.errstate(invalid="ignore"):
+        d = np.where(p > 0, x64 - m, 0.0)
+    mean = np.abs(p * d).sum(1, keepdims=True)
+    s = u * (2 * mean + V / 64 + 72) + 4 * u * np.abs(ls)
+    return s, s * 2 * (1 + mean) + 4 * u * (np.abs(ls) + mean)
+
+
+def check_scores(x, tokens, top, xp=None, entropy=True):
+    """Runs the call on host logits x and holds every output against 64 bits."""
+    rows, V = x.shape
+    xd = xp.view if xp is not None else x.cuda()
+    n = tokens.shape[1] if tokens is not None else 0
+    lp = torch.full((rows, n), float(FILL), device="cuda") if n else None
+    ent = torch.full((rows + 1,), float(FILL), device="cuda")
+    ids = torch.full((rows * top + 1,), FILL, dtype=torch.int32, device="cuda")
+    tlp = torch.full((rows * top + 1,), float(FILL), device="cuda")
+    nbytes = Q.logprobs_workspace_bytes(rows, V, top)
+    work = torch.full((nbytes + 256,), FILL, dtype=torch.int8, device="cuda")
+    Q.token_logprobs(xd, None if not n else tokens.cuda(), lp, ent[:rows] if entropy else None, ids[:-1].view(rows, top) if top else None,
+                     tlp[:-1].view(rows, top) if top else None, work[:nbytes] if nbytes else None)
+    torch.cuda.synchronize()
+    assert ids[-1] == FILL and tlp[-1] == FILL and ent[-1] == FILL and bool((work[nbytes:] == FILL).all())
+    x64 = x.double().numpy()
+    bad = (np.isnan(x64) | (x64 == np.inf)).any(1)
+    none = (x64 == -np.inf).all(1)
+    ok = ~(bad | none)
+    xs = np.where(ok[:, None], x64, 0.0)
+    m = xs.max(1, keepdims=True)
+    e = np.exp(xs - m)
+    s = e.sum(1, keepdims=True)
+    ls = np.log(s)                                       # (m + ls would lose it where m is the type's largest)
+    p = e / s
+    H = -(np.where(p > 0, p, 1) * np.log(np.where(p > 0, p, 1))).sum(1)
+    tol_lp, tol_h = _score_bounds(xs, m, ls, p, V)
+    u = 2.0 ** -24
+
+    def lp_of(t):
+        with np.errstate(invalid="ignore"):
+            v = (np.take_along_axis(x64, t, 1) - m) - ls
+        v = np.where(none[:, None], -np.inf, v)
+        return np.where(bad[:, None], np.nan, v)
+
+    def near(got, want, tol, what):
+        got = got.double().cpu().numpy()
+        fine = np.isfinite(want)
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)]), what
+        off = np.abs(np.where(fine, got, 0) - np.where(fine, want, 0)) - np.broadcast_to(tol, want.shape)
+        assert (off <= 0).all(), f"{what}: {off.max()} over the tolerance"
+
+    if n:
+        t = tokens.long().numpy()
+        want = lp_of(np.clip(t, 0, V - 1))
+        want = np.where(t < 0, 0.0, np.where(t >= V, np.nan, want))
+        with np.errstate(invalid="ignore"):
+            dist = np.abs(np.where(np.isfinite(want), want, 0))
+        near(lp, want, tol_lp + 2 * u * (dist + np.abs(ls)), "log probabilities")
+    if entropy:
+        near(ent[:rows], np.where(bad, np.nan, np.where(none, 0.0, H)), tol_h[:, 0], "entropies")
+    else:
+        assert bool((ent == FILL).all())
+    if top:
+        order = np.argsort(np.where(np.isnan(x64), -np.inf, -x64), axis=1, kind="stable")[:, :top]
+        got = ids[:-1].view(rows, top).cpu().numpy()
+        assert np.array_equal(got, np.where(bad[:, None], -1, order)), "ids of the alternatives"
+        want = lp_of(order)
+        near(tlp[:-1].view(rows, top), want, tol_lp + 2 * u * (np.abs(np.where(np.isfinite(want), want, 0)) + np.abs(ls)), "alternatives")
+
+
+WIDTHS = [1, 2, 3, 29, 63, 64, 65, 100, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1000, 1023, 1024, 1025, 2047, 2048, 2049, 4095, 4096, 4097, 5000, 8191, 8193,
+          16384, 16385, 20000, 32767, 32768, 32769, 50257]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", WIDTHS)
+def test_token_logprobs(V, dtype):
+    g = gen(V)
+    for rows, top, n, pad, shift in ((5, min(V, 5), 1, 0, 0), (3, min(V, 64), 4, 16, 8), (2, 0, 0, 3, 1), (1, min(V, 20), 70, 5, 3)):
+        print(f"[case] logprobs {rows} x {V} {dtype} top {top} tokens {n} pad {pad}", flush=True)
+        x = (torch.randn(rows, V, generator=g) * 4).to(dtype)
+        tokens = torch.randint(0, V, (rows, n), generator=g).int()
+        check_scores(x, tokens if n else None, top, Padded(rows, V, dtype, V + pad, shift, x))
+
+
+@pytest.mark.parametrize("rows,V", [(1, 65536), (2, 100003), (1, 128256), (3, 262144), (1, 1000001), (40, 40000), (700, 3001), (5000, 30)])
+def test_token_logprobs_long_and_many(rows, V):
+    print(f"[case] logprobs {rows} x {V}", flush=True)
+    g = gen(V + rows)
+    for dtype in TYPES:
+        x = (torch.randn(rows, V, generator=g) * 4).to(dtype)
+        check_scores(x, torch.randint(0, V, (rows, 2), generator=g).int(), 20, Padded(rows, V, dtype, V + 1, 1, x) if V % 2 else None)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [70, 1000, 9000, 40000, 140000])
+def test_token_logprobs_values(V, dtype):
+    """Masked rows, ties of every kind, extremes, infinities, NaN, one certain token, tokens out of range."""
+    print(f"[case] logprobs values V={V} {dtype}", flush=True)
+    g, ninf, lowest = gen(V + 3), float("-inf"), torch.finfo(dtype).min
+    x = (torch.randn(20, V, generator=g) * 3).to(dtype)
+    x[1] = 0.0                                           # all equal
+    x[2] = ninf                                          # nothing allowed
+    x[3] = ninf
+    x[3, V - 1] = -4.0                                   # one allowed, the last
+    x[4] = lowest                                        # the type's lowest value everywhere
+    x[5, 10:] = ninf                                     # fewer allowed than asked for
+    x[6, ::3] = lowest
+    x[7, 5] = float("nan")
+    x[8, V - 1] = float("inf")
+    x[9] = float("nan")
+    x[10] = torch.where(torch.arange(V) % 2 == 0, 0.0, -0.0).to(dtype)     # zeros of either sign
+    x[11] = (torch.arange(V) % 7).to(dtype)              # many equal
+    x[12] = torch.arange(V).float().clamp(max=60000).to(dtype)             # growing: the best come last
+    x[13] = -torch.arange(V).float().clamp(max=60000).to(dtype)
+    x[14] = -100.0
+    x[14, 3] = 100.0                                     # certain
+    x[15] = torch.finfo(dtype).max
+    x[16] = ninf
+    x[16, 7], x[16, 60] = 1.5, 1.5
+    x[17, V // 2:] = 50.0                                # half of them best
+    x[18] = 1e-5
+    x[18, 64:] = 2e-5
+    x[19, 0] = ninf
+    tokens = torch.tensor([[0, V - 1, -1, V, 3, -(1 << 31), (1 << 31) - 1, 60]], dtype=torch.int32).repeat(20, 1)
+    for top in (64, 7, 1, 0):
+        check_scores(x, tokens, top)
+    check_scores(x, None, 20, entropy=False)
+
+
+def test_token_logprobs_rows_beyond_32_bits():
+    print("[case] logprobs, offsets beyond 32 bits", flush=True)
+    g = gen(12)
+    rows, V, far = 9, 1000, (1 << 29) + 7
+    x = (torch.randn(rows, V, generator=g) * 4).to(torch.bfloat16)
+    check_scores(x, torch.randint(0, V, (rows, 1), generator=g).int(), 5, Padded(rows, V, torch.bfloat16, far, 3, x))
+
+
+# ---- together, streams, graphs
+
+def _chain(g, T, H, F, E, A, V):
+    """A token's way through a layer, its experts and the last layer to scores: inputs, and the buffers of every call."""
+    c = lambda *s: codes(g, *s).cuda()
+    rows = T * A
+    chosen = torch.rand(T, E, generator=g).topk(A, 1).indices.reshape(-1)
+    order = chosen.sort(stable=True).indices
+    offsets = torch.cat([torch.zeros(1), torch.bincount(chosen, minlength=E).cumsum(0)]).int().cuda()
+    s = dict(x=torch.randn(T, H, generator=g).bfloat16().cuda(), w0=c(H, H), w0s=scales(g, H).cuda() / 20, w1=c(E, F, H),
+             w1s=scales(g, E, F).cuda() / 20, wv=c(V, F), wvs=scales(g, V).cuda() / 20, offsets=offsets, index=(order // A).int().cuda(),
+             tokens=torch.randint(0, V, (rows, 1), generator=g).int().cuda())
+    dev = dict(device="cuda")
+    s |= dict(h=torch.empty(T, H, dtype=torch.bfloat16, **dev), q=torch.empty(T, H, dtype=torch.int8, **dev), qs=torch.empty(T, **dev),
+              f=torch.empty(rows, F, dtype=torch.float16, **dev), lg=torch.empty(rows, V, **dev), lp=torch.empty(rows, 1, **dev),
+              ent=torch.empty(rows, **dev), ids=torch.empty(rows, 8, dtype=torch.int32, **dev), tlp=torch.empty(rows, 8, **dev),
+              ws0=torch.empty(Q.linear_workspace_bytes(T, H), dtype=torch.int8, **dev), ws1=torch.empty(Q.linear_workspace_bytes(rows, F), dtype=torch.int8, **dev),
+              ws2=torch.empty(Q.logprobs_workspace_bytes(rows, V, 8), dtype=torch.int8, **dev))
+    return s
+
+
+def _run_chain(s):
+    Q.linear_int8_dynamic(s["x"], s["w0"], s["w0s"], None, s["h"], s["ws0"])
+    Q.quantize_tokens(s["h"], s["q"], s["qs"])
+    Q.experts_int8(s["q"], s["qs"], s["offsets"], s["index"], s["w1"], s["w1s"], None, s["f"])
+    Q.linear_int8_dynamic(s["f"], s["wv"], s["wvs"], None, s["lg"], s["ws1"])
+    Q.token_logprobs(s["lg"], s["tokens"], s["lp"], s["ent"], s["ids"], s["tlp"], s["ws2"])
+    return {k: s[k] for k in ("h", "q", "qs", "f", "lg", "lp", "ent", "ids", "tlp")}
+
+
+@pytest.mark.parametrize("T,H,F,E,A,V", [(1, 128, 256, 8, 2, 1000), (37, 200, 333, 5, 2, 40001), (300, 256, 512, 16, 4, 2048)])
+def test_chain_of_operators(T, H, F, E, A, V):
+    """The operators one after the other as a program uses them, each held against the definition on the bits that the one before
+    left; again on another stream, and captured and replayed on changed inputs."""
+    print(f"[case] chain T={T} H={H} F={F} E={E} A={A} V={V}", flush=True)
+    s = _chain(gen(T + V), T, H, F, E, A, V)
+
+    def check(o):
+        h = {k: v.cpu() for k, v in {**s, **o}.items()}
+        q0, S0 = quantize_ref(h["x"])
+        same(o["h"], linear_ref(q0, S0, h["w0"], h["w0s"], None, torch.bfloat16), "first layer")
+        q1, S1 = quantize_ref(h["h"])
+        same(o["q"], q1, "codes")
+        same(o["qs"], S1, "scales")
+        same(o["f"], experts_ref(q1, S1, h["offsets"].tolist(), h["index"], h["w1"], h["w1s"], None, torch.zeros(T * A, F, dtype=torch.float16)), "experts")
+        q2, S2 = quantize_ref(h["f"])
+        same(o["lg"], linear_ref(q2, S2, h["wv"], h["wvs"], None, torch.float32), "last layer")
+        x64 = h["lg"].double()
+        lp = torch.log_softmax(x64, 1)
+        assert torch.equal(h["ids"].long(), torch.sort(x64, dim=1, descending=True, stable=True).indices[:, :8])
+        x64, lpn = x64.numpy(), lp.numpy()
+        m = x64.max(1, keepdims=True)
+        ls = np.log(np.exp(x64 - m).sum(1, keepdims=True))
+        tol, _ = _score_bounds(x64, m, ls, np.exp(lpn), V)
+        got = np.take_along_axis(lpn, h["tokens"].long().numpy(), 1)
+        assert (np.abs(h["lp"].double().numpy() - got) <= tol + 2.0 ** -23 * (np.abs(got) + np.abs(ls))).all()
+
+    first = {k: v.clone() for k, v in _run_chain(s).items()}
+    check(first)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = {k: v.clone() for k, v in _run_chain(s).items()}
+    torch.cuda.current_stream().wait_stream(side)
+    for k in first:
+        assert torch.equal(first[k], again[k]), k
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _run_chain(s)
+    for r in range(3):
+        s["x"].copy_(torch.randn(T, H, generator=gen(r)).bfloat16())
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = {k: s[k].clone() for k in first}
+        eager = {k: v.clone() for k, v in _run_chain(s).items()}
+        torch.cuda.synchronize()
+        for k in first:
+            assert torch.equal(replayed[k], eager[k]), (r, k)
+        check(replayed)
+
+
+def test_same_bits_every_time():
+    print("[case] same bits every time", flush=True)
+    s = _chain(gen(4), 64, 256, 512, 8, 2, 5000)
+    first = {k: v.clone() for k, v in _run_chain(s).items()}
+    for _ in range(5):
+        for k in first:
+            s[k].fill_(1)
+        for k, v in _run_chain(s).items():
+            assert torch.equal(v, first[k]), k

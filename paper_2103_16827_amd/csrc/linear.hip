@@ -1,18 +1,34 @@
-// Matrix products of int8 codes with a scale per token and per channel, one matrix or one per group of rows.
+// Matrix products of int8 codes with a scale per token and per channel, one matrix or one per group of rows:
+//   y[m,n] = ((float)(sum_k x[m,k] w[n,k]) x_scale[m]) w_scale[n] + bias[n].
 //
-// A wave computes 16 channels x 16 tokens: the operands of v_mfma_i32_16x16x64_i8 are 16 consecutive bytes of a row per lane
-// (lane = 16 g + r: row r, bytes 16 g .. 16 g + 15 of a chunk of 64), the weights as the first operand, so that a lane
-// ends with four consecutive channels of one token.
+// Both operands are rows of K consecutive codes, which is what v_mfma_i32_16x16x64_i8 wants: lane 16 g + r brings 16
+// consecutive codes of row r (chunk g of 64).  Rows go to LDS by direct loads (1 KiB each) in steps of 64 or 128 codes; the
+// lane of a load that writes slot s of a row brings chunk s ^ f(row), so that the 16-byte reads of an operand (one chunk of
+// many rows) touch every bank once.  Weights are the first operand: a lane ends up with four consecutive channels of one
+// token, and which channels the rows of an operand are is chosen so that a lane has 16 bytes of y over one or two products.
+//
+// linear_few (few tokens): the weights pass once from memory to one workgroup, which is all such a product costs.  The waves
+// of a workgroup split K, each with a ring of its own in LDS and no barrier before the end, where the exact int32
+// partial sums meet in LDS.
+// linear_tile (more): tiles of BM x BN through a ring in LDS that the waves share, a barrier per step.
 #include "floats.hpp"
 #include "kernels.hpp"
 #include "launch_shape.hpp"
+#include "vmem.hpp"
+
+#include <algorithm>
+#include <cmath>
 
 namespace qasr {
 namespace {
 
-typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 
-// bytes [k, k + 16) of a row of K bytes, zeros past its end
+constexpr int kLdsBytes = 160 * 1024;
+
+__device__ __align__(16) const uint8_t kZeros[16] = {};   // what stands for codes past the end of a row
+
+// bytes [k, k + 16) of a row of K bytes, zeros past its end; any alignment
 __device__ __forceinline__ v4i row_chunk(const int8_t* row, int k, int K) {
   if (k + 16 <= K) return *reinterpret_cast<const unaligned_chunk16*>(row + k);
   v4i v = (v4i){0, 0, 0, 0};
@@ -20,76 +36,683 @@ __device__ __forceinline__ v4i row_chunk(const int8_t* row, int k, int K) {
   return v;
 }
 
-// The group and the rows [lo, hi) of tile t where every group's rows are cut into tiles of BM; false past the last tile.
+struct Tile {
+  int e;            // group
+  int lo, hi;       // its rows
+  int n0;           // first channel
+};
+
+// offsets[i] held to [0, M]
+__device__ __forceinline__ int offset_at(const LinearParams& L, int i) { return min(max(L.offsets[i], 0), L.M); }
+
+// How the launch's workgroups are shared out.  Workgroup b runs on XCD b mod 8: an XCD gets consecutive tiles, which read the
+// same rows of x or w, so that these come to its L2 once.
+struct Order {
+  int nt;           // tiles of channels
+  int mt;           // tiles of rows (groups: the most there can be)
+  int along;        // tiles of rows that take turns before the next tile of channels
+};
+
+// the unit-th of n units (fewer than 2^31), in runs of consecutive ones per XCD; -1 past the last
+__device__ __forceinline__ int xcd_order(uint32_t unit, uint32_t n) {
+  const uint32_t per = (n + 7) / 8, t = (unit & 7) * per + (unit >> 3);
+  return (unit >> 3) < per && t < n ? (int)t : -1;
+}
+__device__ __forceinline__ uint32_t first_unit() { return (blockIdx.y << kGridShift) + blockIdx.x; }
+
+// The tile of this workgroup where every group's rows are cut into tiles of BM; false if there is none.  Rows are counted 64
+// groups at a time by a scan over the lanes; every wave does it for itself.
 template <int BM>
-__device__ __forceinline__ bool group_tile(const LinearParams& p, int64_t t, int& e, int& lo, int& hi) {
+__device__ __forceinline__ bool group_tile(const LinearParams& L, const Order& o, uint32_t unit, int BN, Tile& t) {
   const int lane = threadIdx.x & 63;
-  for (int e0 = 0; e0 < p.E; e0 += 64) {
-    int a = 0, b = 0;
-    if (e0 + lane < p.E) {
-      a = min(max(p.offsets[e0 + lane], 0), p.M);
-      b = min(max(p.offsets[e0 + lane + 1], 0), p.M);
-    }
-    const int n = b > a ? (b - a + BM - 1) / BM : 0;
-    int upto = n;                                      // tiles of this and the groups before it among the 64
+  int64_t total = 0;
+  for (int e0 = 0; e0 < L.E; e0 += 64) {
+    const int e = min(e0 + lane, L.E - 1);
+    const int a = offset_at(L, e), b = offset_at(L, e + 1);
+    int n = e0 + lane < L.E && b > a ? (b - a + BM - 1) / BM : 0;
+    for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
+    total += n;
+  }
+  // (more than o.mt only where offsets decrease)
+  const int tiles = __builtin_amdgcn_readfirstlane((int)min(total, (int64_t)o.mt));
+  const int u = xcd_order(unit, (uint32_t)tiles * o.nt);
+  if (u < 0) return false;
+  int left = u / o.nt;
+  t.n0 = (u - left * o.nt) * BN;
+  for (int e0 = 0; e0 < L.E; e0 += 64) {
+    const int e = min(e0 + lane, L.E - 1);
+    const int a = offset_at(L, e), b = offset_at(L, e + 1);
+    const int n = e0 + lane < L.E && b > a ? (b - a + BM - 1) / BM : 0;
+    int upto = n;                           // tiles of this group and of those before it
     for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(upto, d);
-      upto += lane >= d ? o : 0;
+      const int v = __shfl_up(upto, d);
+      upto += lane >= d ? v : 0;
     }
-    const int all = __shfl(upto, 63);
-    if (t < all) {
-      const int src = __popcll(__ballot(upto <= (int)t));
-      e = e0 + src;
-      lo = __shfl(a, src) + ((int)t - __shfl(upto - n, src)) * BM;
-      hi = min(__shfl(b, src), lo + BM);
+    const int all = __builtin_amdgcn_readlane(upto, 63);
+    if (left < all) {
+      const int src = __popcll(__ballot(upto <= left));
+      t.e = e0 + src;
+      t.lo = __shfl(a, src) + (left - __shfl(upto - n, src)) * BM;
+      t.hi = min(__shfl(b, src), t.lo + BM);
       return true;
     }
-    t -= all;
+    left -= all;
   }
   return false;
 }
 
+// the same for one matrix: `along` tiles of rows by all tiles of channels, the rows going first
+template <int BM>
+__device__ __forceinline__ bool plain_tile(const LinearParams& L, const Order& o, uint32_t unit, int BN, Tile& t) {
+  const int u = xcd_order(unit, (uint32_t)o.mt * o.nt);
+  if (u < 0) return false;
+  const int band = u / (o.along * o.nt), in = u - band * o.along * o.nt;
+  const int rows = min(o.along, o.mt - band * o.along), across = in / rows;
+  t.e = 0;
+  t.lo = (band * o.along + in - across * rows) * BM;
+  t.hi = min(L.M, t.lo + BM);
+  t.n0 = across * BN;
+  return true;
+}
+
+template <int BM>
+__device__ __forceinline__ bool find_tile(const LinearParams& L, const Order& o, uint32_t unit, int BN, Tile& t) {
+  if (!L.offsets) return plain_tile<BM>(L, o, unit, BN, t);
+  const bool found = group_tile<BM>(L, o, unit, BN, t);
+  t.e = __builtin_amdgcn_readfirstlane(t.e);
+  t.lo = __builtin_amdgcn_readfirstlane(t.lo);
+  t.hi = __builtin_amdgcn_readfirstlane(t.hi);
+  return found;
+}
+
+// row of x that row m of y reads, -1 for one that is not there
+__device__ __forceinline__ int x_row(const LinearParams& L, int m) {
+  if (!L.index) return m;
+  const int i = L.index[m];
+  return i >= 0 && i < L.x_rows ? i : -1;
+}
+
+// Slot of a row's chunk c is c ^ f: what eight consecutive lanes read of as many rows then lies in different banks.  A row of
+// 128 codes fills the banks, of 64 half of them.  Rows are counted as an operand's lanes read them (r = lane & 15).
+template <int STEP>
+__device__ __forceinline__ int swizzle(int r) { return STEP == 128 ? r & 7 : (r >> 1) & 3; }
+
+// Row r of product nt of a wave is its channel channel_of: lanes 16 g .. end with 4 P consecutive channels of a token over P
+// products, 16 bytes of y.
+template <int P>
+__device__ __forceinline__ int channel_of(int nt, int r) { return 16 * P * (nt / P) + 4 * P * (r >> 2) + 4 * (nt % P) + (r & 3); }
+template <int P>
+__device__ __forceinline__ int row_of(int n) { return 4 * ((n / (4 * P)) & 3) + (n & 3); }      // the r of channel n
+
+// how many products a lane's 16 bytes of y come from
 template <typename T>
-__global__ __launch_bounds__(256) void linear_kernel(LinearParams p, int64_t tiles) {
-  const int64_t unit = (((int64_t)blockIdx.y << kGridShift) + blockIdx.x) * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  if (unit >= tiles) return;
-  const int n16 = (p.N + 15) / 16;
-  const int n0 = (int)(unit % n16) * 16;
-  int e = 0, lo = (int)(unit / n16) * 16, hi = min(p.M, lo + 16);
-  if (p.offsets && !group_tile<16>(p, unit / n16, e, lo, hi)) return;
-  const int m = min(lo + r, hi - 1);
-  int i = p.index ? p.index[m] : m;
-  const bool known = i >= 0 && i < p.x_rows;
-  i = known ? i : 0;
-  const int8_t* wr = p.w + e * p.wes + min(n0 + r, p.N - 1) * p.ws;
-  const int8_t* xr = p.x + i * p.xs;
-  v4i acc = (v4i){0, 0, 0, 0};
-  for (int k = 16 * g; k - 16 * g < p.K; k += 64)
-    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(row_chunk(wr, k, p.K), row_chunk(xr, k, p.K), acc, 0, 0, 0);
-  if (lo + r >= hi) return;
-  const float sx = p.x_scale[i];
-  T* yr = (T*)p.y + (int64_t)m * p.ys;
+constexpr int products_of(int NT) { return NT < 4 / (int)sizeof(T) ? NT : 4 / (int)sizeof(T); }
+
+// each operation rounds once, as the ABI says; the sum itself rounds where it passes 2^24.  No bias is -0: it changes nothing.
+template <typename T>
+__device__ __forceinline__ T result(int acc, float sx, float ws, float bias) {
+#pragma clang fp contract(off)
+  const float v = ((float)acc * sx) * ws;
+  return from_float<T>(v + bias);
+}
+
+// the scale of row m of y's tokens: a row that is not there counts as zeros
+__device__ __forceinline__ float token_scale(const LinearParams& L, int m) {
+  const int xr = x_row(L, m);
+  return xr >= 0 ? L.x_scale[xr] : 0.0f;
+}
+__device__ __forceinline__ float channel_scale(const LinearParams& L, const Tile& t, int n) {
+  return L.w_scale[(int64_t)t.e * L.N + min(n, L.N - 1)];
+}
+__device__ __forceinline__ float channel_bias(const LinearParams& L, const Tile& t, int n) {
+  return L.bias ? L.bias[(int64_t)t.e * L.N + min(n, L.N - 1)] : -0.0f;
+}
+
+// ---- few tokens
+
+// W waves; wave w takes the steps w, w + W, ...; DIRECT: rows 16-byte aligned, K a multiple of 16
+template <int MT, int NT, int W, int S, bool DIRECT, typename T>
+__global__ __launch_bounds__(64 * W) void linear_few_kernel(LinearParams L, Order o) {
+  constexpr int STEP = 128, P = products_of<T>(NT);
+  constexpr int BM = 16 * MT, BN = 16 * NT, kLoads = (BM + BN) / 8, kStage = (BM + BN) * STEP;
+  static_assert(S * kStage >= MT * NT * 1024, "a wave's partial sums go where its ring was");
+  extern __shared__ __align__(1024) unsigned char lds[];
+  Tile t;
+  if (!find_tile<BM>(L, o, first_unit(), BN, t)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  unsigned char* ring = lds + wave * (S * kStage);
+
+  const int steps = (L.K + STEP - 1) / STEP;
+  const int mine = wave < steps ? (steps - wave + W - 1) / W : 0;
+  const int8_t* row[kLoads];
+  int chunk[kLoads];
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const int n = n0 + 4 * g + c;
-    if (n >= p.N) break;
-    const int64_t at = (int64_t)e * p.N + n;
-    float v = __fmul_rn(__fmul_rn((float)(known ? acc[c] : 0), sx), p.w_scale[at]);
-    if (p.bias) v = __fadd_rn(v, p.bias[at]);
-    yr[n] = from_float<T>(v);
+  for (int j = 0; j < kLoads; ++j) {
+    const int i = 8 * j + (lane >> 3);
+    if (8 * j < BM) {
+      const int xr = x_row(L, min(t.lo + i, t.hi - 1));
+      row[j] = L.x + (int64_t)max(xr, 0) * L.xs;
+      chunk[j] = (lane & 7) ^ swizzle<STEP>(i & 15);
+    } else {
+      const int n = i - BM;
+      row[j] = L.w + t.e * L.wes + (int64_t)min(t.n0 + n, L.N - 1) * L.ws;
+      chunk[j] = (lane & 7) ^ swizzle<STEP>(row_of<P>(n));
+    }
+  }
+
+  // At the end every wave puts some of the 16 x 16 results together; what they are scaled by is asked for now.
+  struct Item { int m, n; float sx; v4f ws, bias; };
+  auto item = [&](int i) __attribute__((always_inline)) {
+    Item it;
+    it.m = t.lo + 16 * (i / NT) + r;
+    it.n = t.n0 + channel_of<P>(i % NT, 4 * g);
+    it.sx = token_scale(L, min(it.m, t.hi - 1));
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      it.ws[c] = channel_scale(L, t, it.n + c);
+      it.bias[c] = channel_bias(L, t, it.n + c);
+    }
+    return it;
+  };
+  Item mine_at_end = item(min(wave, MT * NT - 1));
+
+  v4i acc[MT][NT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = (v4i){0, 0, 0, 0};
+
+  auto products = [&](const unsigned char* stage) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = 16 * ((4 * h + g) ^ swizzle<STEP>(r));
+      v4i a[MT], b[NT];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) a[mt] = *(const v4i*)(stage + (16 * mt + r) * STEP + at);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) b[nt] = *(const v4i*)(stage + (BM + channel_of<P>(nt, r)) * STEP + at);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[nt], a[mt], acc[mt][nt], 0, 0, 0);
+    }
+  };
+
+  if constexpr (DIRECT) {
+    auto ask = [&](int i) __attribute__((always_inline)) {
+      const int k0 = (wave + i * W) * STEP;
+      unsigned char* stage = ring + (i % S) * kStage;
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int k = k0 + 16 * chunk[j];
+        const void* p = k < L.K ? (const void*)(row[j] + k) : (const void*)kZeros;
+        direct_load16(p, stage + 1024 * j);
+      }
+    };
+    for (int i = 0; i < min(S, mine); ++i) ask(i);
+    for (int i = 0; i < mine; ++i) {
+      if (i + S <= mine) wait_vm<(S - 1) * kLoads>();
+      else wait_vm_dyn((mine - 1 - i) * kLoads);
+      products(ring + (i % S) * kStage);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the slot has been read
+      if (i + S < mine) ask(i + S);
+    }
+    wait_vm<0>();
+  } else {
+    v4i next[kLoads];
+    auto fetch = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) next[j] = row_chunk(row[j], (wave + i * W) * STEP + 16 * chunk[j], L.K);
+    };
+    if (mine > 0) fetch(0);
+    for (int i = 0; i < mine; ++i) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) *(v4i*)(ring + 1024 * j + 16 * lane) = next[j];
+      if (i + 1 < mine) fetch(i + 1);
+      __builtin_amdgcn_wave_barrier();
+      products(ring);
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) *(v4i*)(ring + (mt * NT + nt) * 1024 + 16 * lane) = acc[mt][nt];
+  __syncthreads();
+#pragma unroll
+  for (int i0 = 0; i0 < MT * NT; i0 += W) {
+    const int i = i0 + wave;
+    if (i >= MT * NT) break;
+    if (i0 > 0) mine_at_end = item(i);
+    const Item& it = mine_at_end;
+    v4i sum = (v4i){0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < W; ++w) sum += *(const v4i*)(lds + w * (S * kStage) + i * 1024 + 16 * lane);
+    if (it.m >= t.hi) continue;
+    T* y = (T*)L.y + (int64_t)it.m * L.ys + it.n;
+    struct __attribute__((packed, aligned(sizeof(T)))) Four { T v[4]; } f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) f.v[c] = result<T>(sum[c], it.sx, it.ws[c], it.bias[c]);
+    if (it.n + 4 <= L.N) {
+      *reinterpret_cast<Four*>(y) = f;
+    } else {
+#pragma unroll
+      for (int c = 0; c < 3; ++c)
+        if (it.n + c < L.N) y[c] = f.v[c];
+    }
+  }
+}
+
+// ---- tiles
+
+template <int MT, int NT>
+using Sums = v4i[MT][NT];
+
+// A wave's 16 MT x 16 NT products over one half (64 codes) of a stage whose tokens begin at `as` and channels at `bs`, at the
+// lane's own row; at: the lane's chunk
+template <int MT, int NT, int P, int STEP>
+__device__ __forceinline__ void products_of_half(Sums<MT, NT>& acc, const unsigned char* as, const unsigned char* bs) {
+  v4i a[MT], b[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) b[nt] = *(const v4i*)(bs + channel_of<P>(nt, 0) * STEP);
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) a[mt] = *(const v4i*)(as + 16 * mt * STEP);
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[nt], a[mt], acc[mt][nt], 0, 0, 0);
+}
+
+// scales in LDS: BM of the tile's tokens, BN of its channels, BN biases
+template <int BM, int BN, int THREADS>
+struct Scales {
+  static constexpr int kEach = (BM + 2 * BN + THREADS - 1) / THREADS;
+  float v[kEach];
+  __device__ __forceinline__ void load(const LinearParams& L, const Tile& t) {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int i = threadIdx.x + j * THREADS;
+      v[j] = i < BM ? token_scale(L, min(t.lo + i, t.hi - 1)) : i < BM + BN ? channel_scale(L, t, t.n0 + i - BM) : channel_bias(L, t, t.n0 + i - BM - BN);
+    }
+  }
+  __device__ __forceinline__ void put(float* to) const {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int i = threadIdx.x + j * THREADS;
+      if (i < BM + 2 * BN) to[i] = v[j];
+    }
+  }
+};
+
+// The results of a wave go through its share (ROOM bytes) of the LDS that the stages were in, as many tokens at a time as fit,
+// so that they leave as whole cache lines: from the registers, where a lane has 16 bytes of every product or two, they would go
+// as 64-byte pieces, which took 8 us more for 4096 x 4096 bf16.  Piece p of a row is at p ^ (row & 7).
+template <int MT, int NT, int BM, int BN, int ROOM, typename T>
+__device__ __forceinline__ void store_tile(const LinearParams& L, const Tile& t, const float* scales, unsigned char* room, int m0, int n0,
+                                           const Sums<MT, NT>& acc) {
+  constexpr int P = products_of<T>(NT), C = 4 * P, PR = NT * (int)sizeof(T);      // C channels are a piece, PR pieces a row
+  constexpr int kFit = ROOM / (16 * PR * 16), MB = kFit >= MT ? MT : kFit >= 4 ? 4 : kFit >= 2 ? 2 : 1;
+  static_assert(C * sizeof(T) == 16 && PR >= 8 && 64 % PR == 0 && MT % MB == 0 && kFit >= 1, "room for rows of pieces");
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  v4f ws[NT], bias[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    ws[nt] = *(const v4f*)(scales + BM + n0 + channel_of<P>(nt, 4 * g));
+    bias[nt] = *(const v4f*)(scales + BM + BN + n0 + channel_of<P>(nt, 4 * g));
+  }
+  const int p = lane % PR, n = t.n0 + n0 + C * p;
+#pragma unroll
+  for (int b = 0; b < MT / MB; ++b) {
+    const int mb = m0 + 16 * MB * b;
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      const float sx = scales[mb + 16 * i + r];
+#pragma unroll
+      for (int j = 0; j < NT / P; ++j) {
+        struct __attribute__((aligned(16))) { T v[C]; } piece;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          piece.v[c] = result<T>(acc[MB * b + i][P * j + c / 4][c % 4], sx, ws[P * j + c / 4][c % 4], bias[P * j + c / 4][c % 4]);
+        *(v4i*)(room + ((16 * i + r) * PR + ((4 * j + g) ^ (r & 7))) * 16) = __builtin_bit_cast(v4i, piece);
+      }
+      __builtin_amdgcn_sched_barrier(0);                     // (else the registers do not last)
+    }
+    asm volatile("" ::: "memory");                           // other lanes read it: a wave's LDS accesses stay in order
+    const int rows = min(16 * MB, t.hi - t.lo - mb);
+    T* y = (T*)L.y + (int64_t)(t.lo + mb) * L.ys + n;
+    if (n + C <= L.N) {
+#pragma unroll 4
+      for (int row = lane / PR; row < rows; row += 64 / PR)
+        *reinterpret_cast<unaligned_chunk16*>(y + row * L.ys) = *(const v4i*)(room + (row * PR + (p ^ (row & 7))) * 16);
+    } else {
+      for (int row = lane / PR; row < rows; row += 64 / PR)
+        for (int c = 0; n + c < L.N; ++c) y[row * L.ys + c] = ((const T*)(room + (row * PR + (p ^ (row & 7))) * 16))[c];
+    }
+    asm volatile("" ::: "memory");
+  }
+}
+
+// WM x WN waves of 16 MT tokens x 16 NT channels each, S stages of 128 codes.
+template <int MT, int NT, int WM, int WN, int S, typename T>
+__global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearParams L, Order o) {
+  constexpr int STEP = 128, P = products_of<T>(NT), RPL = 1024 / STEP, CPR = STEP / 16;     // rows per load, chunks per row
+  constexpr int W = WM * WN, BM = 16 * MT * WM, BN = 16 * NT * WN, kStage = (BM + BN) * STEP;
+  constexpr int kTokenLoads = BM / RPL / W, kLoads = kTokenLoads + BN / RPL / W;
+  static_assert(BM % (RPL * W) == 0 && BN % (RPL * W) == 0, "whole loads of tokens and of channels for every wave");
+  static_assert(RPL * W % 16 == 0, "a lane brings the same chunk in all its loads of tokens, and in all of channels");
+  static_assert(MT >= 2 && S * kStage + 4 * (BM + 2 * BN) <= kLdsBytes, "LDS");
+  extern __shared__ __align__(1024) unsigned char lds[];
+  float* scales = (float*)(lds + S * kStage);
+  Tile t;
+  if (!find_tile<BM>(L, o, first_unit(), BN, t)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const int wm = wave / WN, wn = wave % WN;
+  const int steps = (L.K + STEP - 1) / STEP;
+
+  // the rows that this lane brings, by 32-bit offsets from the tile's first rows (the launch sees to it that these do)
+  const int first = RPL * wave + lane / CPR;
+  const int token_chunk = (lane % CPR) ^ swizzle<STEP>(first & 15), channel_chunk = (lane % CPR) ^ swizzle<STEP>(row_of<P>(first));
+  const int8_t* xbase = L.x + (L.index ? 0 : (int64_t)t.lo * L.xs);
+  const int8_t* wbase = L.w + t.e * L.wes + (int64_t)t.n0 * L.ws;
+  uint32_t off[kLoads];
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const int i = first + RPL * W * (j < kTokenLoads ? j : j - kTokenLoads);
+    const int m = min(i, t.hi - t.lo - 1);
+    if (j < kTokenLoads) off[j] = (uint32_t)(L.index ? max(x_row(L, t.lo + m), 0) : m) * (uint32_t)L.xs + 16 * token_chunk;
+    else off[j] = (uint32_t)min(i, L.N - 1 - t.n0) * (uint32_t)L.ws + 16 * channel_chunk;
+  }
+  // load j of stage k, which goes to `slot`; past the end of a row come zeros of the tokens (ask_end), anything of the channels
+  auto ask_one = [&](int k, int slot, int j) __attribute__((always_inline)) {
+    const int left = L.K - k * STEP;
+    if (16 * (j < kTokenLoads ? token_chunk : channel_chunk) < left)
+      direct_load16((j < kTokenLoads ? xbase : wbase) + k * STEP, off[j], lds + slot + 1024 * (j * W + wave));
+  };
+  auto ask_end = [&](int k, int slot) __attribute__((always_inline)) {
+    if (16 * token_chunk >= L.K - k * STEP) {
+#pragma unroll
+      for (int j = 0; j < kTokenLoads; ++j) *(v4i*)(lds + slot + 1024 * (j * W + wave) + 16 * lane) = (v4i){0, 0, 0, 0};
+    }
+  };
+  // Two halves of a stage take turns, each one's operands read under the products of the one before.  Once the second
+  // half's are on their way into registers, and the next stage has come, the stage's room is free: it is asked for again there.
+  Sums<MT, NT> acc;
+  v4i a[MT], b[2][NT];
+  const int at[2] = {16 * (g ^ swizzle<STEP>(r)), 16 * ((4 + g) ^ swizzle<STEP>(r))};
+  const unsigned char* as = lds + (16 * MT * wm + r) * STEP;
+  const unsigned char* bs = lds + (BM + 16 * NT * wn + channel_of<P>(0, r)) * STEP;
+  auto read_a = [&](int mt, int slot, int h) __attribute__((always_inline)) { a[mt] = *(const v4i*)(as + slot + at[h] + 16 * mt * STEP); };
+  auto read_b = [&](int nt, int slot, int h) __attribute__((always_inline)) { b[h][nt] = *(const v4i*)(bs + slot + at[h] + channel_of<P>(nt, 0) * STEP); };
+  auto read_bs = [&](int mt, int slot, int h) __attribute__((always_inline)) {
+    if (mt < NT) read_b(mt, slot, h);
+    if (mt == MT - 1) {
+#pragma unroll
+      for (int nt = MT; nt < NT; ++nt) read_b(nt, slot, h);
+    }
+  };
+  auto products_of_row = [&](int mt, int h) __attribute__((always_inline)) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[h][nt], a[mt], acc[mt][nt], 0, 0, 0);
+  };
+  auto first_half = [&](int slot) __attribute__((always_inline)) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      products_of_row(mt, 0);
+      read_a(mt, slot, 1);
+      read_bs(mt, slot, 1);
+      __builtin_amdgcn_sched_barrier(0);           // (else the reads come early and the registers do not last)
+    }
+  };
+  auto second_half = [&](int next, auto&& among) __attribute__((always_inline)) {
+    read_a(0, next, 0);
+    read_b(0, next, 0);
+#pragma unroll
+    for (int mt = 1; mt < MT; ++mt) {
+      among(mt);
+      products_of_row(mt, 1);
+      read_a(mt, next, 0);
+      read_bs(mt, next, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  Scales<BM, BN, 64 * W> sc;
+  sc.load(L, t);
+#pragma unroll 1
+  for (int k = 0; k < min(S, steps); ++k) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) ask_one(k, k * kStage, j);
+    ask_end(k, k * kStage);
+  }
+  sc.put(scales);
+  if (steps >= S) wait_vm<(S - 1) * kLoads>();
+  else wait_vm<0>();
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) read_b(nt, 0, 0);
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) read_a(mt, 0, 0);
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = (v4i){0, 0, 0, 0};
+  int slot = 0, k = 0;
+  // while the stage to ask for is a whole one: no branches among the products
+  const int8_t *xk = xbase + S * STEP, *wk = wbase + S * STEP;
+  for (const int whole = L.K / STEP; k + S < whole; ++k) {
+    const int next = slot + kStage == S * kStage ? 0 : slot + kStage;
+    first_half(slot);
+    products_of_row(0, 1);
+    wait_vm<(S - 2) * kLoads>();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    second_half(next, [&](int mt) __attribute__((always_inline)) {
+      // (the requests of a step, a few at a time: a wave whose request has to queue issues no products meanwhile)
+#pragma unroll
+      for (int j = kLoads * (mt - 1) / (MT - 1); j < kLoads * mt / (MT - 1); ++j)
+        direct_load16(j < kTokenLoads ? xk : wk, off[j], lds + slot + 1024 * (j * W + wave));
+    });
+    xk += STEP;
+    wk += STEP;
+    slot = next;
+  }
+  for (; k + 1 < steps; ++k) {
+    const int next = slot + kStage == S * kStage ? 0 : slot + kStage;
+    first_half(slot);
+    products_of_row(0, 1);
+    if (k + S - 1 < steps) wait_vm<(S - 2) * kLoads>();
+    else wait_vm<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (k + S < steps) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) ask_one(k + S, slot, j);
+      ask_end(k + S, slot);
+    }
+    second_half(next, [](int) {});
+    slot = next;
+  }
+  first_half(slot);
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    products_of_row(mt, 1);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");     // every stage has been read
+  store_tile<MT, NT, BM, BN, S * kStage / W, T>(L, t, scales, lds + S * kStage / W * wave, 16 * MT * wm, 16 * NT * wn, acc);
+  wait_vm<0>();
+}
+
+// The same tiles where rows begin anywhere or end inside a chunk: rows come through registers.
+template <int MT, int NT, int WM, int WN, typename T>
+__global__ __launch_bounds__(64 * WM * WN) void linear_rows_kernel(LinearParams L, Order o) {
+  constexpr int STEP = 128, P = products_of<T>(NT), RPL = 1024 / STEP, CPR = STEP / 16;
+  constexpr int W = WM * WN, BM = 16 * MT * WM, BN = 16 * NT * WN, kStage = (BM + BN) * STEP;
+  constexpr int kTokenLoads = BM / RPL / W, kLoads = kTokenLoads + BN / RPL / W;
+  static_assert(BM % (RPL * W) == 0 && BN % (RPL * W) == 0 && RPL * W % 16 == 0, "see linear_tile_kernel");
+  extern __shared__ __align__(1024) unsigned char lds[];
+  float* scales = (float*)(lds + 2 * kStage);
+  Tile t;
+  if (!find_tile<BM>(L, o, first_unit(), BN, t)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int wm = wave / WN, wn = wave % WN, steps = (L.K + STEP - 1) / STEP;
+  const int first = RPL * wave + lane / CPR;
+  const int token_chunk = (lane % CPR) ^ swizzle<STEP>(first & 15), channel_chunk = (lane % CPR) ^ swizzle<STEP>(row_of<P>(first));
+  const int8_t* row[kLoads];
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const int i = first + RPL * W * (j < kTokenLoads ? j : j - kTokenLoads);
+    if (j < kTokenLoads) row[j] = L.x + (int64_t)max(x_row(L, min(t.lo + i, t.hi - 1)), 0) * L.xs;
+    else row[j] = L.w + t.e * L.wes + (int64_t)min(t.n0 + i, L.N - 1) * L.ws;
+  }
+  Scales<BM, BN, 64 * W> sc;
+  sc.load(L, t);
+  v4i next[kLoads];
+  auto fetch = [&](int k) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) next[j] = row_chunk(row[j], k * STEP + 16 * (j < kTokenLoads ? token_chunk : channel_chunk), L.K);
+  };
+  auto put = [&](unsigned char* stage) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) *(v4i*)(stage + 1024 * (j * W + wave) + 16 * lane) = next[j];
+  };
+  Sums<MT, NT> acc;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = (v4i){0, 0, 0, 0};
+  fetch(0);
+  put(lds);
+  sc.put(scales);
+  __syncthreads();
+  for (int k = 0; k < steps; ++k) {
+    const unsigned char* stage = lds + (k & 1) * kStage;
+    if (k + 1 < steps) fetch(k + 1);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = 16 * ((4 * h + g) ^ swizzle<STEP>(r));
+      products_of_half<MT, NT, P, STEP>(acc, stage + (16 * MT * wm + r) * STEP + at, stage + (BM + 16 * NT * wn + channel_of<P>(0, r)) * STEP + at);
+    }
+    if (k + 1 < steps) put(lds + ((k + 1) & 1) * kStage);
+    __syncthreads();
+  }
+  store_tile<MT, NT, BM, BN, 2 * kStage / W, T>(L, t, scales, lds + 2 * kStage / W * wave, 16 * MT * wm, 16 * NT * wn, acc);
+}
+
+// ---- launches
+
+// tiles of BM rows (groups: the most that the rows can make)
+int64_t row_tiles(const LinearParams& p, int BM) {
+  return p.offsets ? p.M / BM + (p.E < p.M ? p.E : p.M) : ((int64_t)p.M + BM - 1) / BM;
+}
+
+Order order_of(const LinearParams& p, int BM, int BN) { return Order{(p.N + BN - 1) / BN, (int)row_tiles(p, BM), 8}; }
+
+GridShape grid_of(const Order& o) { return grid_shape(((int64_t)o.mt * o.nt + 7) / 8 * 8); }
+
+template <int MT, int NT, int W, int S, bool DIRECT, typename T>
+hipError_t launch_few(const LinearParams& p, hipStream_t st) {
+  const Order o = order_of(p, 16 * MT, 16 * NT);
+  const GridShape g = grid_of(o);
+  constexpr int bytes = W * S * 16 * (MT + NT) * 128;
+  static std::atomic<uint64_t> done;
+  const hipError_t e = ensure_max_dynamic_lds((const void*)linear_few_kernel<MT, NT, W, S, DIRECT, T>, done);
+  if (e != hipSuccess) return e;
+  return launch_kernel(linear_few_kernel<MT, NT, W, S, DIRECT, T>, dim3(g.x, g.y), dim3(64 * W), bytes, st, p, o);
+}
+
+template <int MT, int NT, int WM, int WN, int S, typename T>
+hipError_t launch_tile(const LinearParams& p, hipStream_t st) {
+  constexpr int BM = 16 * MT * WM, BN = 16 * NT * WN, bytes = S * (BM + BN) * 128 + 4 * (BM + 2 * BN);
+  const Order o = order_of(p, BM, BN);
+  const GridShape g = grid_of(o);
+  static std::atomic<uint64_t> done;
+  const hipError_t e = ensure_max_dynamic_lds((const void*)linear_tile_kernel<MT, NT, WM, WN, S, T>, done);
+  if (e != hipSuccess) return e;
+  return launch_kernel(linear_tile_kernel<MT, NT, WM, WN, S, T>, dim3(g.x, g.y), dim3(64 * WM * WN), bytes, st, p, o);
+}
+
+template <int MT, int NT, int WM, int WN, typename T>
+hipError_t launch_rows(const LinearParams& p, hipStream_t st) {
+  constexpr int BM = 16 * MT * WM, BN = 16 * NT * WN, bytes = 2 * (BM + BN) * 128 + 4 * (BM + 2 * BN);
+  const Order o = order_of(p, BM, BN);
+  const GridShape g = grid_of(o);
+  static std::atomic<uint64_t> done;
+  const hipError_t e = ensure_max_dynamic_lds((const void*)linear_rows_kernel<MT, NT, WM, WN, T>, done);
+  if (e != hipSuccess) return e;
+  return launch_kernel(linear_rows_kernel<MT, NT, WM, WN, T>, dim3(g.x, g.y), dim3(64 * WM * WN), bytes, st, p, o);
+}
+
+// Rows on 16-byte boundaries that hold whole chunks, and whose offsets within a tile (with an index: within x) are 32-bit numbers.
+bool direct_ok(const LinearParams& p) {
+  if (p.K % 16 || p.xs % 16 || p.ws % 16 || p.wes % 16 || (uintptr_t)p.x % 16 || (uintptr_t)p.w % 16) return false;
+  const int64_t most = ((int64_t)1 << 32) - 1024;
+  return p.ws < most / 256 && (p.index ? p.xs < most / p.x_rows : p.xs < most / 256);
+}
+
+// What a form of the kernels takes for one tile on a compute unit, in us: `end` for its beginning and end, `alone` for a step of 128
+// codes with nothing else on the chip, `busy` with a tile on every unit.  Fitted to 22 shapes of 1 to 4096 tokens on weights that
+// are not in a cache; next to the fastest form of each shape, what the rule takes cost 0 to 10 % more.
+struct Form { int BM, BN, per_unit; double end, alone, busy; };
+constexpr Form kForms[] = {
+    {16, 16, 2, 0.15, 0.09, 0.0535},   // linear_few, from here
+    {32, 32, 2, 0.3, 0.12, 0.106},
+    {32, 64, 1, 0.4, 0.17, 0.2},
+    {64, 64, 1, 0.5, 0.24, 0.35},
+    {64, 128, 2, 2.0, 0.29, 0.375},    // linear_tile, from here
+    {128, 128, 1, 2.0, 0.40, 0.65},
+    {128, 256, 1, 3.0, 0.57, 1.0},
+    {256, 256, 1, 5.5, 1.1, 1.7},
+};
+constexpr int kFormCount = sizeof(kForms) / sizeof(kForms[0]);
+
+// tiles of BM rows that a launch will have: for groups, of which only the device knows the sizes, as if rows fell on them by chance
+double expected_row_tiles(const LinearParams& p, int BM) {
+  if (!p.offsets) return (double)row_tiles(p, BM);
+  const double busy = p.E * (1.0 - std::pow(1.0 - 1.0 / p.E, (double)p.M)), rows = p.M / busy;
+  return busy * (rows <= BM / 2 ? 1.0 : rows / BM + 0.5);
+}
+
+int fastest_form(const LinearParams& p) {
+  const double steps = (p.K + 127) / 128, units = compute_units();
+  int best = 0;
+  double least = 0;
+  for (int i = 0; i < kFormCount; ++i) {
+    const Form& f = kForms[i];
+    const double tiles = expected_row_tiles(p, f.BM) * ((p.N + f.BN - 1) / f.BN), load = tiles / units;
+    const double us = std::max(std::ceil(load / f.per_unit) * (f.end + steps * f.alone),
+                               (load > 1 ? std::ceil(load) : std::sqrt(std::sqrt(load))) * (f.end + steps * f.busy));
+    if (i == 0 || us < least) {
+      best = i;
+      least = us;
+    }
+  }
+  return best;
+}
+
+template <typename T>
+hipError_t launch_typed(const LinearParams& p, hipStream_t st) {
+  if (!direct_ok(p)) {
+    const double rows = p.offsets ? (double)p.M / p.E : p.M;
+    if (rows <= 16) return launch_few<1, 1, 8, 1, false, T>(p, st);
+    if (rows <= 64) return launch_few<4, 2, 4, 1, false, T>(p, st);
+    return launch_rows<4, 4, 2, 2, T>(p, st);
+  }
+  switch (fastest_form(p)) {
+    case 0: return launch_few<1, 1, 8, 2, true, T>(p, st);
+    case 1: return launch_few<2, 2, 4, 2, true, T>(p, st);
+    case 2: return launch_few<2, 4, 4, 2, true, T>(p, st);
+    case 3: return launch_few<4, 4, 4, 2, true, T>(p, st);
+    case 4: return launch_tile<2, 4, 2, 2, 3, T>(p, st);
+    case 5: return launch_tile<4, 4, 2, 2, 4, T>(p, st);
+    case 6: return launch_tile<4, 4, 2, 4, 3, T>(p, st);
+    default: return launch_tile<8, 4, 2, 4, 2, T>(p, st);
   }
 }
 
 }  // namespace
 
 hipError_t launch_linear(const LinearParams& p, hipStream_t st) {
-  const int64_t m16 = p.offsets ? p.M / 16 + (p.E < p.M ? p.E : p.M) : (p.M + 15) / 16;
-  const int64_t tiles = m16 * ((p.N + 15) / 16);
-  const GridShape g = grid_shape((tiles + 3) / 4);
-  return with_type(p.y_type, [&](auto t) {
-    return launch_kernel(linear_kernel<decltype(t)>, dim3(g.x, g.y), dim3(256), 0, st, p, tiles);
-  });
+  return with_type(p.y_type, [&](auto t) { return launch_typed<decltype(t)>(p, st); });
 }
 
 }  // namespace qasr

@@ -4,16 +4,19 @@
 // it once into registers.  From there:
 //   - the maximum m, then s = sum e^(x - m) and t = sum e^(x - m) (x - m): ln s gives the log probabilities, ln s - t / s the
 //     entropy.  Two sweeps over registers instead of a running maximum: one exponential per logit and no rescaling.
-//   - the alternatives by a threshold: lane l of every wave owns the logits of column l of the 64, and the `top`-th largest of
-//     the 64 columns' maxima is reached by at least `top` logits, and hardly more where the best are spread by chance.  Those
-//     are gathered in LDS and ranked by counting.  Where more reach it than there is room for (equal logits, mostly), the
-//     best are taken out one after the other instead.
+//   - the alternatives by a threshold.  Threads are columns, 64 of them or four times as many (some threads each): the `top`-th
+//     largest of the columns' maxima is reached by `top` logits at least, and hardly more where the best are spread by
+//     chance.  The few threads whose maximum reaches it put their logits in LDS, where all threads look for those
+//     that do; these are ranked by counting.  Where they are too many for the room (thousands of equal logits), the best are
+//     taken out one after the other, from memory.
 // Pieces leave (m, s, t) and their best in the workspace; a second kernel joins them.
-// What bounds it: the logits' way from memory, and next to it about ten vector operations per logit, of which the exponential
-// takes four times the others' time.
+// What bounds it: the logits' way from memory, and next to it about eleven vector operations per logit, of which the
+// exponential takes four times the others' time.
 #include "floats.hpp"
 #include "kernels.hpp"
 #include "launch_shape.hpp"
+
+#include <type_traits>
 
 namespace qasr {
 namespace {
@@ -21,7 +24,7 @@ namespace {
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
 constexpr int kMaxTop = 64;
-constexpr int kRoom = 256;          // candidates that are ranked at once
+constexpr int kRoom = 512;          // candidates that are ranked at once
 
 // order of a float as an unsigned number; zeros of either sign are equal
 __device__ __forceinline__ uint32_t order_of(float v) {
@@ -32,20 +35,50 @@ __device__ __forceinline__ float value_of(uint32_t o) { return __builtin_bit_cas
 // larger logits first, equal ones by the lower id; 0 is below every logit
 __device__ __forceinline__ uint64_t key_of(float v, int id) { return (uint64_t)order_of(v) << 32 | (uint32_t)~id; }
 
+// Reductions over the lanes, by moves among them that are part of the operation (a shuffle through LDS costs a round trip each):
+// within rows of 16, then across them.  The result is in every lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lane_move(uint32_t keep, uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)keep, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <typename V, typename Op>
+__device__ __forceinline__ V wave_reduce(V v, V none, Op op) {
+  auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
+    constexpr int C = decltype(ctrl)::value, R = decltype(rows)::value;
+    if constexpr (sizeof(V) == 8) {
+      const uint64_t n = __builtin_bit_cast(uint64_t, none), b = __builtin_bit_cast(uint64_t, v);
+      const uint64_t o = (uint64_t)lane_move<C, R>((uint32_t)(n >> 32), (uint32_t)(b >> 32)) << 32 | lane_move<C, R>((uint32_t)n, (uint32_t)b);
+      v = op(v, __builtin_bit_cast(V, o));
+    } else {
+      v = op(v, __builtin_bit_cast(V, lane_move<C, R>(__builtin_bit_cast(uint32_t, none), __builtin_bit_cast(uint32_t, v))));
+    }
+  };
+  using std::integral_constant;
+  step(integral_constant<int, 0x111>(), integral_constant<int, 0xf>());      // from the lanes 1, 2, 4, 8 before it in its row of 16
+  step(integral_constant<int, 0x112>(), integral_constant<int, 0xf>());
+  step(integral_constant<int, 0x114>(), integral_constant<int, 0xf>());
+  step(integral_constant<int, 0x118>(), integral_constant<int, 0xf>());
+  step(integral_constant<int, 0x142>(), integral_constant<int, 0xa>());      // the last of a row to the row after it (rows 1 and 3)
+  step(integral_constant<int, 0x143>(), integral_constant<int, 0xc>());      // the last of the second row to the third and fourth
+  if constexpr (sizeof(V) == 8) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(V, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), 63) << 32 |
+                                     (uint32_t)__builtin_amdgcn_readlane((int)b, 63));
+  } else {
+    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+  }
+}
 __device__ __forceinline__ float wave_max(float v) {
-  for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+  return wave_reduce(v, -__builtin_inff(), [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float wave_sum(float v) {
-  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+  return wave_reduce(v, 0.0f, [](float a, float b) { return a + b; });
 }
 __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-  for (int d = 32; d > 0; d >>= 1) {
-    const uint64_t o = __shfl_xor((unsigned long long)v, d);
-    v = o > v ? o : v;
-  }
-  return v;
+  return wave_reduce(v, (uint64_t)0, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+}
+__device__ __forceinline__ uint32_t wave_min(uint32_t v) {
+  return wave_reduce(v, ~0u, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
 }
 
 // Logits per 16 bytes, and the e-th of them
@@ -76,34 +109,35 @@ struct Pieces {
   uint64_t* best;    // [rows][n][top]
 };
 
-// the outputs of a row from its (m, s, t); its alternatives' keys, best first, in `best`
-template <typename T>
-__device__ __forceinline__ void finish(const LogprobParams& p, int64_t row, float m, float s, float t, const uint64_t* best, int tid, int threads) {
-  const float ninf = -__builtin_inff(), nan = __builtin_nanf("");
-  const bool bad = s != s, none = s == 0.0f;           // a NaN or +infinity; nothing but -infinity
-  const float base = none ? 0.0f : m, ls = __logf(s);
-  auto score = [&](float x) { return bad ? nan : none ? ninf : (x - base) - ls; };
-  const T* x = (const T*)p.x + row * p.xs;
-  for (int j = tid; j < p.n; j += threads) {
-    const int tok = p.tokens[row * p.n + j];
-    p.logprob[row * p.n + j] = tok < 0 ? 0.0f : tok >= p.V ? nan : score(to_float(x[tok]));
+// the outputs of a row from its (m, s, t)
+struct Scorer {
+  float base, ls, entropy;
+  bool bad, none;              // a NaN or +infinity; nothing but -infinity
+  __device__ __forceinline__ Scorer(float m, float s, float t) {
+    bad = s != s;
+    none = s == 0.0f;
+    base = none ? 0.0f : m;
+    ls = __logf(s);
+    entropy = bad ? __builtin_nanf("") : none ? 0.0f : ls - t / s;
   }
-  if (tid == 0 && p.entropy) p.entropy[row] = bad ? nan : none ? 0.0f : ls - t / s;
-  if (tid < p.top) {
-    const uint64_t k = best[tid];
-    p.top_ids[row * p.top + tid] = bad ? -1 : (int)~(uint32_t)k;
-    p.top_logprob[row * p.top + tid] = score(value_of((uint32_t)(k >> 32)));
+  __device__ __forceinline__ float operator()(float x) const {
+    return bad ? __builtin_nanf("") : none ? -__builtin_inff() : (x - base) - ls;
   }
-}
-
-// LDS of a choice of the best
-template <int W>
-struct Choice {
-  uint32_t column[64];               // the largest number in each column
-  uint64_t cand[kRoom];
-  uint64_t best[kMaxTop];            // the outcome, best first
-  uint64_t wave_best[W];
-  int count;
+  // the entropy and the given tokens' scores
+  template <typename T>
+  __device__ __forceinline__ void tokens(const LogprobParams& p, int64_t row, int tid, int threads) const {
+    const T* x = (const T*)p.x + row * p.xs;
+    for (int j = tid; j < p.n; j += threads) {
+      const int tok = p.tokens[row * p.n + j];
+      p.logprob[row * p.n + j] = tok < 0 ? 0.0f : tok >= p.V ? __builtin_nanf("") : (*this)(to_float(x[tok]));
+    }
+    if (tid == 0 && p.entropy) p.entropy[row] = entropy;
+  }
+  // the alternative of rank j
+  __device__ __forceinline__ void alternative(const LogprobParams& p, int64_t row, int j, uint64_t key) const {
+    p.top_ids[row * p.top + j] = bad ? -1 : (int)~(uint32_t)key;
+    p.top_logprob[row * p.top + j] = (*this)(value_of((uint32_t)(key >> 32)));
+  }
 };
 
 template <int W>
@@ -112,80 +146,111 @@ __device__ __forceinline__ void sync() {
   else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-// The `top` largest of the keys that W waves hold, at least that many.  own: the order of the thread's largest; each(limit, f)
-// calls f(key) for each of its keys of an order of `limit` or more, or for more of them.  c.column and c.count were cleared, with a sync
-// after that.
-template <int W, typename Each>
-__device__ __forceinline__ void choose(Choice<W>& c, int top, uint32_t own, int tid, Each&& each) {
-  const int lane = tid & 63;
-  atomicMax(&c.column[lane], own);
-  sync<W>();
-  // the largest number that at least `top` of the columns reach, bit by bit (every wave for itself)
-  const uint32_t mine = c.column[lane];
-  uint32_t limit = 0;
-  if (top < 64) {
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t higher = limit | 1u << bit;
-      if (__popcll(__ballot(mine >= higher)) >= top) limit = higher;
+// LDS of a choice of the best: the largest number in each column, and the candidates
+template <int W>
+struct Choice {
+  static constexpr int kQuarters = W >= 4 ? 4 : 1;     // columns / 64, where `top` is large
+  uint32_t column[64 * kQuarters];
+  uint64_t cand[kRoom];
+  uint64_t wave_best[W];
+  int count, holders;
+
+  __device__ __forceinline__ void clear(int tid) {
+    if (tid < 64) {
+#pragma unroll
+      for (int q = 0; q < kQuarters; ++q) column[64 * q + tid] = 0;
     }
-  } else {
-    limit = mine;
-    for (int d = 32; d > 0; d >>= 1) limit = min(limit, (uint32_t)__shfl_xor((int)limit, d));
+    if (tid == 0) count = holders = 0;
   }
-  if (own >= limit) {
-    each(limit, [&](uint64_t key) {
-      const int to = atomicAdd(&c.count, 1);
-      if (to < kRoom) c.cand[to] = key;
-    });
+  // own: the order of the thread's largest.  (A sync comes before it and after it.)
+  __device__ __forceinline__ void offer(int top, uint32_t own, int tid) {
+    atomicMax(&column[(tid & 63) + (top > 24 ? 64 * ((tid >> 6) % kQuarters) : 0)], own);
   }
-  sync<W>();
-  const int found = c.count;
-  if (found <= kRoom) {
+  // The largest number, in its first BITS bits, that at least `top` of the columns reach, bit by bit (every wave for itself).  64
+  // columns have at least that many; where there are fewer, all of them count.
+  template <int BITS>
+  __device__ __forceinline__ uint32_t limit(int top) const {
+    const int lane = threadIdx.x & 63;
+    uint32_t mine[kQuarters], found = 0;
+#pragma unroll
+    for (int q = 0; q < kQuarters; ++q) mine[q] = top > 24 || q == 0 ? column[64 * q + lane] : 0;
+    for (int bit = 31; bit >= 32 - BITS; --bit) {
+      const uint32_t higher = found | 1u << bit;
+      int n = 0;
+#pragma unroll
+      for (int q = 0; q < kQuarters; ++q) n += __popcll(__ballot(mine[q] >= higher));
+      if (n >= top) found = higher;
+    }
+    return found;
+  }
+  __device__ __forceinline__ void add(uint64_t key) {
+    const int to = atomicAdd(&count, 1);
+    if (to < kRoom) cand[to] = key;
+  }
+  // Calls f(rank, key) for the `top` best candidates.  (A sync comes before it.)
+  template <typename F>
+  __device__ __forceinline__ void rank(int top, int tid, F&& f) const {
+    const int found = count;
     for (int i = tid; i < found; i += 64 * W) {
-      const uint64_t k = c.cand[i];
-      int rank = 0;
-      for (int o = 0; o < found; ++o) rank += c.cand[o] > k;
-      if (rank < top) c.best[rank] = k;
+      const uint64_t k = cand[i];
+      int r = 0;
+      for (int o = 0; o < found; ++o) r += cand[o] > k;
+      if (r < top) f(r, k);
     }
-  } else {
-    // one after the other: every thread offers its best that is still to come
+  }
+  // The same for all keys next(i), i = tid, tid + 64 W .. < n, one after the other
+  template <typename Next, typename F>
+  __device__ __forceinline__ void one_by_one(int top, int n, int tid, Next&& next, F&& f) {
     uint64_t last = ~0ull;
     for (int j = 0; j < top; ++j) {
       uint64_t b = 0;
-      each(0, [&](uint64_t key) { b = key < last && key > b ? key : b; });
+#pragma unroll 1
+      for (int i = tid; i < n; i += 64 * W) {
+        const uint64_t key = next(i);
+        b = key < last && key > b ? key : b;
+      }
       b = wave_max(b);
       if constexpr (W > 1) {
         sync<W>();
-        if (lane == 0) c.wave_best[tid >> 6] = b;
+        if ((tid & 63) == 0) wave_best[tid >> 6] = b;
         sync<W>();
 #pragma unroll
-        for (int w = 0; w < W; ++w) b = c.wave_best[w] > b ? c.wave_best[w] : b;
+        for (int w = 0; w < W; ++w) b = wave_best[w] > b ? wave_best[w] : b;
       }
       last = b;
-      if (tid == 0) c.best[j] = b;
+      if (tid == 0) f(j, b);
     }
   }
-  sync<W>();
-}
+};
 
 // W waves a row or piece, R loads of 16 bytes a lane: up to 64 W R kPer logits.  W == 1: four rows a workgroup, a wave each.
 template <typename T, int W, int R>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(LogprobParams p, Pieces c) {
   constexpr int N = kPer<T>, kRows = W == 1 ? 4 : 1;
+  constexpr int kHolders = W == 1 ? 32 : 128;          // threads whose logits fit the LDS at once
+  constexpr int BITS = sizeof(T) == 4 ? 20 : __is_same(T, bf16) ? 16 : 19;     // of a logit's order (float32: near enough)
   __shared__ float part[kRows][3 * W];
   __shared__ Choice<W> choices[kRows];
+  __shared__ v4u held[kRows][kHolders * R];
+  __shared__ float held_last[kRows][kHolders];
+  __shared__ int holder[kRows][kHolders];
   const int sub = W == 1 ? threadIdx.x >> 6 : 0;       // the row among the workgroup's
   const int tid = W == 1 ? threadIdx.x & 63 : threadIdx.x, lane = threadIdx.x & 63, wave = tid >> 6;
   const int64_t unit = (((int64_t)blockIdx.y << kGridShift) + blockIdx.x) * kRows + sub;
   if (unit >= p.rows * c.n) return;                    // (W == 1: no barriers below)
-  const int64_t row = c.n == 1 ? unit : unit / c.n;
-  const int piece = c.n == 1 ? 0 : (int)(unit - row * c.n);
+  int64_t row = unit;
+  int piece = 0;
+  if (c.n > 1) {
+    row = unit >> 31 ? unit / c.n : (int64_t)((uint32_t)unit / (uint32_t)c.n);
+    piece = (int)(unit - row * c.n);
+  }
   const int v0 = piece * c.len, len = min(c.len, p.V - v0);
   const T* x = (const T*)p.x + row * p.xs + v0;
   Choice<W>& choice = choices[sub];
+  const int top = min(p.top, len);                     // (a piece may be shorter than p.top)
 
-  const float ninf = -__builtin_inff();
   // Whole loads, and what is left of the row, a logit for each of the first threads.  Lanes past the end hold -infinity.
+  const float ninf = -__builtin_inff();
   const int loads = len / N, rest = loads * N + tid;
   struct __attribute__((packed, aligned(sizeof(T)))) Load { v4u v; };
   v4u raw[R];
@@ -196,30 +261,46 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
     if (i * 64 * W + tid < loads) raw[i] = reinterpret_cast<const Load*>(x + (i * 64 * W + tid) * N)->v;
   }
   const float last = rest < len ? to_float(x[rest]) : ninf;
-  // calls f(a, b, place of a, whether they are logits) for the lane's logits, two neighbours at a time
+  if (top > 0) {
+    choice.clear(tid);
+    sync<W>();                                         // (the logits are on their way)
+  }
+  // calls f(a, b) for the lane's logits, two neighbours at a time
   auto sweep = [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       asm volatile("" : "+v"(raw[i]));                 // (taken apart anew in every sweep: as floats they would need up to twice the registers)
       if (i * 64 * W < loads) {
 #pragma unroll
-        for (int k = 0; k < N; k += 2) f(logit<T>(raw[i], k), logit<T>(raw[i], k + 1), (i * 64 * W + tid) * N + k, i * 64 * W + tid < loads);
+        for (int k = 0; k < N; k += 2) f(logit<T>(raw[i], k), logit<T>(raw[i], k + 1));
       }
     }
   };
   float m = last;
-  sweep([&](float a, float b, int, bool) { m = max3(m, a, b); });
-  const float own = m;                                 // of this thread's logits
+  sweep([&](float a, float b) { m = max3(m, a, b); });
+  const uint32_t own = order_of(m);                    // of this thread's logits
   m = wave_max(m);
-  if (p.top > 0) {
-    if (tid < 64) choice.column[lane] = 0;
-    if (tid == 0) choice.count = 0;
-  }
+  if (top > 0) choice.offer(top, own, tid);
   if constexpr (W > 1) {
     if (lane == 0) part[0][wave] = m;
-    sync<W>();
+  }
+  sync<W>();
+  if constexpr (W > 1) {
 #pragma unroll
     for (int w = 0; w < W; ++w) m = fmaxf(m, part[0][w]);
+  }
+  uint32_t limit = 0;
+  if (top > 0) {
+    limit = choice.template limit<BITS>(top);
+    if (own >= limit && (tid < loads || rest < len)) {
+      const int h = atomicAdd(&choice.holders, 1);
+      if (h < kHolders) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) held[sub][h * R + i] = raw[i];
+        held_last[sub][h] = last;
+        holder[sub][h] = tid;
+      }
+    }
   }
   const float base = m == ninf ? 0.0f : m;             // (nothing but -infinity: every exponential is 0)
   float s = 0.0f, t = 0.0f;
@@ -228,7 +309,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
     s += e;
     t = fmaf(e, fmaxf(d, -1000.0f), t);                // (not 0 times -infinity)
   };
-  sweep([&](float a, float b, int, bool) {
+  sweep([&](float a, float b) {
     add(a);
     add(b);
   });
@@ -240,18 +321,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
       part[0][W + wave] = s;
       part[0][2 * W + wave] = t;
     }
-    if (p.top == 0) sync<W>();                         // (else the choice has one)
   }
-  const int top = min(p.top, len);                     // (a piece may be shorter than that)
-  if (p.top > 0)
-    choose<W>(choice, top, order_of(own), tid, [&](uint32_t limit, auto&& f) __attribute__((always_inline)) {
-      const float least = limit == 0 ? ninf : value_of(limit);
-      sweep([&](float a, float b, int at, bool there) {
-        if (!(a < least) && there) f(key_of(a, v0 + at));
-        if (!(b < least) && there) f(key_of(b, v0 + at + 1));
-      });
-      if (!(last < least) && rest < len) f(key_of(last, v0 + rest));
-    });
+  sync<W>();
   if constexpr (W > 1) {
     s = t = 0.0f;
 #pragma unroll
@@ -260,27 +331,52 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
       t += part[0][2 * W + w];
     }
   }
-  if (c.n == 1) {
-    finish<T>(p, row, m, s, t, choice.best, tid, 64 * W);
-    return;
+  const Scorer score(m, s, t);
+  if (c.n == 1) score.template tokens<T>(p, row, tid, 64 * W);
+  else if (tid == 0) c.part[unit] = Part{m, s, t};
+  if (top == 0) return;
+
+  auto leave = [&](int j, uint64_t key) __attribute__((always_inline)) {
+    if (c.n == 1) score.alternative(p, row, j, key);
+    else c.best[unit * p.top + j] = key;
+  };
+  const int holders = choice.holders;
+  if (holders <= kHolders) {
+    // a load of a holder for each thread, then the holders' last logits
+    for (int i = tid; i < holders * R; i += 64 * W) {
+      const int h = i / R, at = ((i % R) * 64 * W + holder[sub][h]);
+      const v4u v = held[sub][i];
+      if (at < loads) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const float f = logit<T>(v, k);
+          if (order_of(f) >= limit) choice.add(key_of(f, v0 + at * N + k));
+        }
+      }
+    }
+    for (int h = tid; h < holders; h += 64 * W)
+      if (loads * N + holder[sub][h] < len && order_of(held_last[sub][h]) >= limit) choice.add(key_of(held_last[sub][h], v0 + loads * N + holder[sub][h]));
+    sync<W>();
   }
-  if (tid == 0) c.part[unit] = Part{m, s, t};
-  if (tid < p.top) c.best[unit * p.top + tid] = tid < top ? choice.best[tid] : 0;
+  if (holders <= kHolders && choice.count <= kRoom) choice.rank(top, tid, leave);
+  else choice.one_by_one(top, len, tid, [&](int i) { return key_of(to_float(x[i]), v0 + i); }, leave);
+  if (c.n > 1 && tid >= top && tid < p.top) c.best[unit * p.top + tid] = 0;
 }
 
 // A workgroup joins the pieces of a row.
 constexpr int kJoinWaves = 4, kHeld = 16;              // keys that a thread holds
 template <typename T>
 __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(LogprobParams p, Pieces c) {
-  __shared__ Choice<kJoinWaves> choice;
+  constexpr int W = kJoinWaves;
+  __shared__ Choice<W> choice;
   const int64_t row = ((int64_t)blockIdx.y << kGridShift) + blockIdx.x;
   if (row >= p.rows) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const uint64_t* keys = c.best + row * c.n * p.top;
-  const int64_t n = (int64_t)c.n * p.top;
+  const int n = c.n * p.top;
   uint64_t held[kHeld];
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) held[i] = i * 64 * kJoinWaves + tid < n ? keys[i * 64 * kJoinWaves + tid] : 0;
+  for (int i = 0; i < kHeld; ++i) held[i] = i * 64 * W + tid < n ? keys[i * 64 * W + tid] : 0;
   const float ninf = -__builtin_inff();
   float m = ninf;
   for (int i = lane; i < c.n; i += 64) m = fmaxf(m, c.part[row * c.n + i].m);
@@ -296,22 +392,31 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(LogprobParams p, 
   }
   s = wave_sum(s);
   t = wave_sum(t);
-  if (p.top > 0) {
-    if (tid < 64) choice.column[lane] = 0;
-    if (tid == 0) choice.count = 0;
-    sync<kJoinWaves>();
-    auto each = [&](uint32_t limit, auto&& f) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i)
-        if (held[i] != 0 && (uint32_t)(held[i] >> 32) >= limit) f(held[i]);
-      for (int64_t i = kHeld * 64 * kJoinWaves + tid; i < n; i += 64 * kJoinWaves)
-        if (keys[i] != 0 && (uint32_t)(keys[i] >> 32) >= limit) f(keys[i]);
-    };
-    uint64_t own = 0;
-    each(0, [&](uint64_t k) { own = k > own ? k : own; });
-    choose<kJoinWaves>(choice, p.top, (uint32_t)(own >> 32), tid, each);
+  const Scorer score(m, s, t);
+  score.template tokens<T>(p, row, tid, 64 * W);
+  if (p.top == 0) return;
+  auto leave = [&](int j, uint64_t key) __attribute__((always_inline)) { score.alternative(p, row, j, key); };
+  if (n > kHeld * 64 * W) {
+    choice.one_by_one(p.top, n, tid, [&](int i) { return keys[i]; }, leave);
+    return;
   }
-  finish<T>(p, row, m, s, t, choice.best, tid, 64 * kJoinWaves);
+  choice.clear(tid);
+  sync<W>();
+  uint64_t own = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) own = held[i] > own ? held[i] : own;
+  choice.offer(p.top, (uint32_t)(own >> 32), tid);
+  sync<W>();
+  // (columns without a key, or too few of them: the limit is 0 and every key is a candidate)
+  const uint32_t limit = choice.template limit<20>(p.top);
+  if ((uint32_t)(own >> 32) >= limit) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (held[i] != 0 && (uint32_t)(held[i] >> 32) >= limit) choice.add(held[i]);
+  }
+  sync<W>();
+  if (choice.count <= kRoom) choice.rank(p.top, tid, leave);
+  else choice.one_by_one(p.top, n, tid, [&](int i) { return keys[i]; }, leave);
 }
 
 int size_of(int type) { return type == 0 ? 4 : 2; }

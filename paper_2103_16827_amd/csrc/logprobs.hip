@@ -150,10 +150,11 @@ __device__ __forceinline__ void sync() {
 template <int W>
 struct Choice {
   static constexpr int kQuarters = W >= 4 ? 4 : 1;     // columns / 64, where `top` is large
-  uint32_t column[64 * kQuarters];
+  __align__(16) uint32_t column[64 * kQuarters];
   uint64_t cand[kRoom];
   uint64_t wave_best[W];
   int count, holders;
+  uint32_t least;                    // what limit() said
 
   __device__ __forceinline__ void clear(int tid) {
     if (tid < 64) {
@@ -166,15 +167,23 @@ struct Choice {
   __device__ __forceinline__ void offer(int top, uint32_t own, int tid) {
     atomicMax(&column[(tid & 63) + (top > 24 ? 64 * ((tid >> 6) % kQuarters) : 0)], own);
   }
-  // The largest number, in its first BITS bits, that at least `top` of the columns reach, bit by bit (every wave for itself).  64
-  // columns have at least that many; where there are fewer, all of them count.
-  template <int BITS>
+  // One wave: the largest number that at least `top` of the columns reach (in its first 20 bits where there are four times 64).
   __device__ __forceinline__ uint32_t limit(int top) const {
     const int lane = threadIdx.x & 63;
+    if (top <= 24 || kQuarters == 1) {
+      const uint32_t mine = column[lane];
+      int above = 0;
+#pragma unroll 2
+      for (int o = 0; o < 64; o += 4) {
+        const v4u c = *reinterpret_cast<const v4u*>(column + o);
+        above += (c[0] > mine) + (c[1] > mine) + (c[2] > mine) + (c[3] > mine);
+      }
+      return wave_min(above < top ? mine : ~0u);
+    }
     uint32_t mine[kQuarters], found = 0;
 #pragma unroll
-    for (int q = 0; q < kQuarters; ++q) mine[q] = top > 24 || q == 0 ? column[64 * q + lane] : 0;
-    for (int bit = 31; bit >= 32 - BITS; --bit) {
+    for (int q = 0; q < kQuarters; ++q) mine[q] = column[64 * q + lane];
+    for (int bit = 31; bit >= 12; --bit) {
       const uint32_t higher = found | 1u << bit;
       int n = 0;
 #pragma unroll
@@ -214,8 +223,7 @@ struct Choice {
         sync<W>();
         if ((tid & 63) == 0) wave_best[tid >> 6] = b;
         sync<W>();
-#pragma unroll
-        for (int w = 0; w < W; ++w) b = wave_best[w] > b ? wave_best[w] : b;
+        b = wave_max(wave_best[tid % W]);
       }
       last = b;
       if (tid == 0) f(j, b);
@@ -225,10 +233,9 @@ struct Choice {
 
 // W waves a row or piece, R loads of 16 bytes a lane: up to 64 W R kPer logits.  W == 1: four rows a workgroup, a wave each.
 template <typename T, int W, int R>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(LogprobParams p, Pieces c) {
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 16 ? 8 : 1) void logprobs_kernel(LogprobParams p, Pieces c) {
   constexpr int N = kPer<T>, kRows = W == 1 ? 4 : 1;
   constexpr int kHolders = W == 1 ? 32 : 128;          // threads whose logits fit the LDS at once
-  constexpr int BITS = sizeof(T) == 4 ? 20 : __is_same(T, bf16) ? 16 : 19;     // of a logit's order (float32: near enough)
   __shared__ float part[kRows][3 * W];
   __shared__ Choice<W> choices[kRows];
   __shared__ v4u held[kRows][kHolders * R];
@@ -249,16 +256,18 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
   Choice<W>& choice = choices[sub];
   const int top = min(p.top, len);                     // (a piece may be shorter than p.top)
 
-  // Whole loads, and what is left of the row, a logit for each of the first threads.  Lanes past the end hold -infinity.
+  // Whole loads from a 16-byte boundary on, and what is before and behind them, a logit for each of the first threads.  Lanes
+  // past the end hold -infinity.  (Loads that straddle boundaries ran at three quarters of the rate.)
   const float ninf = -__builtin_inff();
-  const int loads = len / N, rest = loads * N + tid;
-  struct __attribute__((packed, aligned(sizeof(T)))) Load { v4u v; };
+  const int head = min(len, (int)(-(uintptr_t)x & 15) / (int)sizeof(T));
+  const int loads = (len - head) / N, rest = tid < head ? tid : loads * N + tid;
+  const v4u* aligned = reinterpret_cast<const v4u*>(x + head);
   v4u raw[R];
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : __is_same(T, bf16) ? 0xff80ff80u : 0xfc00fc00u;
     raw[i] = (v4u){kNone, kNone, kNone, kNone};
-    if (i * 64 * W + tid < loads) raw[i] = reinterpret_cast<const Load*>(x + (i * 64 * W + tid) * N)->v;
+    if (i * 64 * W + tid < loads) raw[i] = aligned[i * 64 * W + tid];
   }
   const float last = rest < len ? to_float(x[rest]) : ninf;
   if (top > 0) {
@@ -285,22 +294,10 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
     if (lane == 0) part[0][wave] = m;
   }
   sync<W>();
-  if constexpr (W > 1) {
-#pragma unroll
-    for (int w = 0; w < W; ++w) m = fmaxf(m, part[0][w]);
-  }
-  uint32_t limit = 0;
-  if (top > 0) {
-    limit = choice.template limit<BITS>(top);
-    if (own >= limit && (tid < loads || rest < len)) {
-      const int h = atomicAdd(&choice.holders, 1);
-      if (h < kHolders) {
-#pragma unroll
-        for (int i = 0; i < R; ++i) held[sub][h * R + i] = raw[i];
-        held_last[sub][h] = last;
-        holder[sub][h] = tid;
-      }
-    }
+  if constexpr (W > 1) m = wave_max(part[0][lane % W]);
+  if (top > 0 && (W == 1 || wave == 0)) {              // (meanwhile the others go on)
+    const uint32_t l = choice.limit(top);
+    if (lane == 0) choice.least = l;
   }
   const float base = m == ninf ? 0.0f : m;             // (nothing but -infinity: every exponential is 0)
   float s = 0.0f, t = 0.0f;
@@ -324,17 +321,24 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
   }
   sync<W>();
   if constexpr (W > 1) {
-    s = t = 0.0f;
+    s = wave_sum(lane < W ? part[0][W + lane] : 0.0f);
+    t = wave_sum(lane < W ? part[0][2 * W + lane] : 0.0f);
+  }
+  const uint32_t limit = top > 0 ? choice.least : 0;
+  if (top > 0 && own >= limit && (tid < loads || rest < len)) {
+    const int h = atomicAdd(&choice.holders, 1);
+    if (h < kHolders) {
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      s += part[0][W + w];
-      t += part[0][2 * W + w];
+      for (int i = 0; i < R; ++i) held[sub][h * R + i] = raw[i];
+      held_last[sub][h] = last;
+      holder[sub][h] = tid;
     }
   }
   const Scorer score(m, s, t);
   if (c.n == 1) score.template tokens<T>(p, row, tid, 64 * W);
   else if (tid == 0) c.part[unit] = Part{m, s, t};
   if (top == 0) return;
+  sync<W>();
 
   auto leave = [&](int j, uint64_t key) __attribute__((always_inline)) {
     if (c.n == 1) score.alternative(p, row, j, key);
@@ -350,12 +354,14 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
 #pragma unroll
         for (int k = 0; k < N; ++k) {
           const float f = logit<T>(v, k);
-          if (order_of(f) >= limit) choice.add(key_of(f, v0 + at * N + k));
+          if (order_of(f) >= limit) choice.add(key_of(f, v0 + head + at * N + k));
         }
       }
     }
-    for (int h = tid; h < holders; h += 64 * W)
-      if (loads * N + holder[sub][h] < len && order_of(held_last[sub][h]) >= limit) choice.add(key_of(held_last[sub][h], v0 + loads * N + holder[sub][h]));
+    for (int h = tid; h < holders; h += 64 * W) {
+      const int at = holder[sub][h] < head ? holder[sub][h] : loads * N + holder[sub][h];
+      if (at < len && order_of(held_last[sub][h]) >= limit) choice.add(key_of(held_last[sub][h], v0 + at));
+    }
     sync<W>();
   }
   if (holders <= kHolders && choice.count <= kRoom) choice.rank(top, tid, leave);
@@ -407,8 +413,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(LogprobParams p, 
   for (int i = 0; i < kHeld; ++i) own = held[i] > own ? held[i] : own;
   choice.offer(p.top, (uint32_t)(own >> 32), tid);
   sync<W>();
-  // (columns without a key, or too few of them: the limit is 0 and every key is a candidate)
-  const uint32_t limit = choice.template limit<20>(p.top);
+  // (where fewer columns than that have a key the limit is 0 and every key is a candidate)
+  const uint32_t limit = choice.limit(p.top);
   if ((uint32_t)(own >> 32) >= limit) {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)

@@ -370,16 +370,17 @@ def softmax_int32(e: IExp, x, y):
 
 
 # ---- language-model operators.  The library sees addresses alone, so what a tensor knows of itself is held against the
-# call here: a type, shape or stride that the call cannot mean, or another GPU than the current one, is a ValueError.
+# call here: a type, shape or stride that the call cannot mean, or another GPU than the current one, is a ValueError.  (These
+# checks are a good part of what a small call costs: shapes and strides are looked at once, in one expression where they can be.)
 _types = None
 
 
 def _torch_types():
-    global _types
-    if _types is None:
-        import torch
-        _types = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.int8: torch.int8,
-                  torch.int32: torch.int32, "int8": torch.int8, "int32": torch.int32, "f32": torch.float32}
+    global _types, _int8, _int32, _f32, _here
+    import torch
+    _int8, _int32, _f32 = torch.int8, torch.int32, torch.float32
+    _types = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+    _here = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     return _types
 
 
@@ -388,45 +389,48 @@ def _refuse(what, t, want):
 
 
 def _float_type(t, what):
-    k = _torch_types().get(t.dtype)
-    if k.__class__ is not int:
+    k = (_types or _torch_types()).get(t.dtype)
+    if k is None:
         _refuse(what, t, "float32, float16 or bfloat16")
     return k
 
 
 def _rows(t, shape, what):
     """The row stride of a matrix (0: dense) whose rows are contiguous."""
+    if t.shape != shape:
+        _refuse(what, t, shape)
+    if t.is_contiguous():
+        return 0
     st = t.stride()
-    if tuple(t.shape) != shape or (st[1] != 1 and shape[1] > 1) or (st[0] < shape[1] and shape[0] > 1):
+    if (st[1] != 1 and shape[1] > 1) or (st[0] < shape[1] and shape[0] > 1):
         _refuse(what, t, f"a {shape} matrix of contiguous rows that do not overlap")
     return st[0] if shape[0] > 1 else 0
 
 
 def _codes(t, shape, what):
-    if t.dtype is not _torch_types()["int8"]:
+    _types or _torch_types()
+    if t.dtype is not _int8:
         _refuse(what, t, "int8")
     return _rows(t, shape, what)
 
 
-def _dense(t, kind, shape, what):
-    if t.dtype is not _torch_types()[kind] or tuple(t.shape) != shape or not t.is_contiguous():
-        _refuse(what, t, f"a dense {kind} tensor of {shape}")
+def _dense(t, dtype, shape, what):
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(what, t, f"a dense {dtype} tensor of {shape}")
 
 
-def _on_device(*tensors):
+def _on_device(x, *others):
     """The current stream, for tensors that are all on the current device."""
-    on = {t.get_device() for t in tensors if t is not None}
-    if len(on) != 1 or -1 in on:
-        raise ValueError(f"tensors on one GPU wanted, got {[str(t.device) for t in tensors if t is not None]}")
+    on = x.get_device()
+    for t in others:
+        if t is not None and t.get_device() != on:
+            raise ValueError(f"tensors on one GPU wanted, got {x.device} and {t.device}")
+    if on < 0:
+        raise ValueError("tensors on a GPU wanted, got tensors in host memory")
     stream = _stream()
-    if _current_device() not in on:
-        raise ValueError(f"the tensors are on cuda:{on.pop()}, the current device is cuda:{_current_device()}")
+    if _here() != on:
+        raise ValueError(f"the tensors are on cuda:{on}, the current device is cuda:{_here()}")
     return stream
-
-
-def _current_device():
-    import torch
-    return torch._C._cuda_getDevice()
 
 
 def _bytes(t):
@@ -437,7 +441,7 @@ def quantize_tokens(x, q, scale):
     """qasr_quantize_tokens: float [M, K] -> int8 codes q [M, K] and float32 scale [M], one per row."""
     M, K = x.shape
     kind, xs, qs = _float_type(x, "x"), _rows(x, (M, K), "x"), _codes(q, (M, K), "q")
-    _dense(scale, "f32", (M,), "scale")
+    _dense(scale, _f32, (M,), "scale")
     stream = _on_device(x, q, scale)
     _check(lib().qasr_quantize_tokens(x.data_ptr(), kind, M, K, xs, q.data_ptr(), qs, scale.data_ptr(), stream),
            "qasr_quantize_tokens")
@@ -446,9 +450,9 @@ def quantize_tokens(x, q, scale):
 
 def _linear_desc(M, N, K, xs, w, w_scale, bias, y):
     ws = _codes(w, (N, K), "w")
-    _dense(w_scale, "f32", (N,), "w_scale")
+    _dense(w_scale, _f32, (N,), "w_scale")
     if bias is not None:
-        _dense(bias, "f32", (N,), "bias")
+        _dense(bias, _f32, (N,), "bias")
     return LinearDesc(M, N, K, _float_type(y, "y"), xs, ws, _rows(y, (M, N), "y"), 0)
 
 
@@ -456,7 +460,7 @@ def linear_int8(x, x_scale, w, w_scale, bias, y):
     """qasr_linear_int8: codes x [M, K] and w [N, K] with scales [M] and [N] (and bias [N] or None) -> float y [M, N]."""
     (M, K), N = x.shape, w.shape[0]
     d = _linear_desc(M, N, K, _codes(x, (M, K), "x"), w, w_scale, bias, y)
-    _dense(x_scale, "f32", (M,), "x_scale")
+    _dense(x_scale, _f32, (M,), "x_scale")
     stream = _on_device(x, x_scale, w, w_scale, bias, y)
     _check(lib().qasr_linear_int8(ctypes.byref(d), x.data_ptr(), x_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), _ptr(bias),
                                   y.data_ptr(), stream), "qasr_linear_int8")
@@ -486,16 +490,16 @@ def experts_int8(x, x_scale, offsets, index, w, w_scale, bias, y):
         M = index.shape[0]
         y = y[:M]
     xs, st = _codes(x, (rows, K), "x"), w.stride()
-    if w.dim() != 3 or w.dtype is not _torch_types()["int8"] or w.shape[2] != K or (st[2] != 1 and K > 1) or \
+    if w.dim() != 3 or w.dtype is not _int8 or w.shape[2] != K or (st[2] != 1 and K > 1) or \
             (st[1] < K and N > 1) or (st[0] < st[1] * (N - 1) + K and E > 1):
         _refuse("w", w, f"int8 of ({E}, {N}, {K}) with contiguous rows that do not overlap")
-    _dense(x_scale, "f32", (rows,), "x_scale")
-    _dense(w_scale, "f32", (E, N), "w_scale")
-    _dense(offsets, "int32", (E + 1,), "offsets")
+    _dense(x_scale, _f32, (rows,), "x_scale")
+    _dense(w_scale, _f32, (E, N), "w_scale")
+    _dense(offsets, _int32, (E + 1,), "offsets")
     if index is not None:
-        _dense(index, "int32", (M,), "index")
+        _dense(index, _int32, (M,), "index")
     if bias is not None:
-        _dense(bias, "f32", (E, N), "bias")
+        _dense(bias, _f32, (E, N), "bias")
     d = ExpertsDesc(LinearDesc(M, N, K, _float_type(y, "y"), xs, st[1] if N > 1 else 0, _rows(y, (M, N), "y"), 0), E, rows,
                     st[0] if E > 1 else 0)
     stream = _on_device(x, x_scale, offsets, index, w, w_scale, bias, y)
@@ -518,15 +522,15 @@ def token_logprobs(x, tokens=None, logprob=None, entropy=None, top_ids=None, top
     if tokens is not None or logprob is not None:
         if tokens is None or logprob is None:
             raise ValueError("tokens and logprob go together")
-        _dense(tokens, "int32", (rows, n), "tokens")
-        _dense(logprob, "f32", (rows, n), "logprob")
+        _dense(tokens, _int32, (rows, n), "tokens")
+        _dense(logprob, _f32, (rows, n), "logprob")
     if entropy is not None:
-        _dense(entropy, "f32", (rows,), "entropy")
+        _dense(entropy, _f32, (rows,), "entropy")
     if top_ids is not None or top_logprob is not None:
         if top_ids is None or top_logprob is None:
             raise ValueError("top_ids and top_logprob go together")
-        _dense(top_ids, "int32", (rows, top), "top_ids")
-        _dense(top_logprob, "f32", (rows, top), "top_logprob")
+        _dense(top_ids, _int32, (rows, top), "top_ids")
+        _dense(top_logprob, _f32, (rows, top), "top_logprob")
     stream = _on_device(x, tokens, logprob, entropy, top_ids, top_logprob, workspace)
     _check(lib().qasr_token_logprobs(x.data_ptr(), kind, rows, V, xs, _ptr(tokens), n, _ptr(logprob), _ptr(entropy), top,
                                      _ptr(top_ids), _ptr(top_logprob), _ptr(workspace), _bytes(workspace), stream),

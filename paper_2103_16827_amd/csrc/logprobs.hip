@@ -14,9 +14,8 @@
 // exponential takes four times the others' time.
 #include "floats.hpp"
 #include "kernels.hpp"
+#include "lanes.hpp"
 #include "launch_shape.hpp"
-
-#include <type_traits>
 
 namespace qasr {
 namespace {
@@ -34,52 +33,6 @@ __device__ __forceinline__ uint32_t order_of(float v) {
 __device__ __forceinline__ float value_of(uint32_t o) { return __builtin_bit_cast(float, o >> 31 ? o & 0x7fffffffu : ~o); }
 // larger logits first, equal ones by the lower id; 0 is below every logit
 __device__ __forceinline__ uint64_t key_of(float v, int id) { return (uint64_t)order_of(v) << 32 | (uint32_t)~id; }
-
-// Reductions over the lanes, by moves among them that are part of the operation (a shuffle through LDS costs a round trip each):
-// within rows of 16, then across them.  The result is in every lane.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t lane_move(uint32_t keep, uint32_t v) {
-  return (uint32_t)__builtin_amdgcn_update_dpp((int)keep, (int)v, CTRL, ROWS, 0xf, false);
-}
-template <typename V, typename Op>
-__device__ __forceinline__ V wave_reduce(V v, V none, Op op) {
-  auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
-    constexpr int C = decltype(ctrl)::value, R = decltype(rows)::value;
-    if constexpr (sizeof(V) == 8) {
-      const uint64_t n = __builtin_bit_cast(uint64_t, none), b = __builtin_bit_cast(uint64_t, v);
-      const uint64_t o = (uint64_t)lane_move<C, R>((uint32_t)(n >> 32), (uint32_t)(b >> 32)) << 32 | lane_move<C, R>((uint32_t)n, (uint32_t)b);
-      v = op(v, __builtin_bit_cast(V, o));
-    } else {
-      v = op(v, __builtin_bit_cast(V, lane_move<C, R>(__builtin_bit_cast(uint32_t, none), __builtin_bit_cast(uint32_t, v))));
-    }
-  };
-  using std::integral_constant;
-  step(integral_constant<int, 0x111>(), integral_constant<int, 0xf>());      // from the lanes 1, 2, 4, 8 before it in its row of 16
-  step(integral_constant<int, 0x112>(), integral_constant<int, 0xf>());
-  step(integral_constant<int, 0x114>(), integral_constant<int, 0xf>());
-  step(integral_constant<int, 0x118>(), integral_constant<int, 0xf>());
-  step(integral_constant<int, 0x142>(), integral_constant<int, 0xa>());      // the last of a row to the row after it (rows 1 and 3)
-  step(integral_constant<int, 0x143>(), integral_constant<int, 0xc>());      // the last of the second row to the third and fourth
-  if constexpr (sizeof(V) == 8) {
-    const uint64_t b = __builtin_bit_cast(uint64_t, v);
-    return __builtin_bit_cast(V, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), 63) << 32 |
-                                     (uint32_t)__builtin_amdgcn_readlane((int)b, 63));
-  } else {
-    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
-  }
-}
-__device__ __forceinline__ float wave_max(float v) {
-  return wave_reduce(v, -__builtin_inff(), [](float a, float b) { return fmaxf(a, b); });
-}
-__device__ __forceinline__ float wave_sum(float v) {
-  return wave_reduce(v, 0.0f, [](float a, float b) { return a + b; });
-}
-__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-  return wave_reduce(v, (uint64_t)0, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
-}
-__device__ __forceinline__ uint32_t wave_min(uint32_t v) {
-  return wave_reduce(v, ~0u, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
-}
 
 // Logits per 16 bytes, and the e-th of them
 template <typename T>
@@ -109,6 +62,18 @@ struct Pieces {
   uint64_t* best;    // [rows][n][top]
 };
 
+// a given token and its logit
+struct Ahead {
+  int tok = -1;
+  float x = 0.0f;
+  template <typename T>
+  __device__ __forceinline__ void load(const LogprobParams& p, int64_t row, int j) {
+    if (j >= p.n) return;
+    tok = p.tokens[row * p.n + j];
+    if (tok >= 0 && tok < p.V) x = to_float(((const T*)p.x + row * p.xs)[tok]);
+  }
+};
+
 // the outputs of a row from its (m, s, t)
 struct Scorer {
   float base, ls, entropy;
@@ -123,13 +88,12 @@ struct Scorer {
   __device__ __forceinline__ float operator()(float x) const {
     return bad ? __builtin_nanf("") : none ? -__builtin_inff() : (x - base) - ls;
   }
-  // the entropy and the given tokens' scores
+  // the entropy and the given tokens' scores; `ahead`: the thread's first token, asked for when the kernel began
   template <typename T>
-  __device__ __forceinline__ void tokens(const LogprobParams& p, int64_t row, int tid, int threads) const {
-    const T* x = (const T*)p.x + row * p.xs;
+  __device__ __forceinline__ void tokens(const LogprobParams& p, int64_t row, int tid, int threads, Ahead ahead) const {
     for (int j = tid; j < p.n; j += threads) {
-      const int tok = p.tokens[row * p.n + j];
-      p.logprob[row * p.n + j] = tok < 0 ? 0.0f : tok >= p.V ? __builtin_nanf("") : (*this)(to_float(x[tok]));
+      if (j != tid) ahead.load<T>(p, row, j);
+      p.logprob[row * p.n + j] = ahead.tok < 0 ? 0.0f : ahead.tok >= p.V ? __builtin_nanf("") : (*this)(ahead.x);
     }
     if (tid == 0 && p.entropy) p.entropy[row] = entropy;
   }
@@ -270,6 +234,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 16 ? 8 : 1) void logpro
     if (i * 64 * W + tid < loads) raw[i] = aligned[i * 64 * W + tid];
   }
   const float last = rest < len ? to_float(x[rest]) : ninf;
+  Ahead ahead;
+  if (c.n == 1) ahead.load<T>(p, row, tid);
   if (top > 0) {
     choice.clear(tid);
     sync<W>();                                         // (the logits are on their way)
@@ -335,7 +301,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 16 ? 8 : 1) void logpro
     }
   }
   const Scorer score(m, s, t);
-  if (c.n == 1) score.template tokens<T>(p, row, tid, 64 * W);
+  if (c.n == 1) score.template tokens<T>(p, row, tid, 64 * W, ahead);
   else if (tid == 0) c.part[unit] = Part{m, s, t};
   if (top == 0) return;
   sync<W>();
@@ -369,6 +335,69 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 16 ? 8 : 1) void logpro
   if (c.n > 1 && tid >= top && tid < p.top) c.best[unit * p.top + tid] = 0;
 }
 
+// Rows of up to G = 16, 32 or 64 logits: a lane each, 64 / G rows a wave.  Reductions by exchanges within the row's lanes; the
+// alternatives one after the other, or their ranks by comparing every logit with all.
+template <int G, typename V, typename Op>
+__device__ __forceinline__ V row_reduce(V v, Op op) {
+  auto moved = [&](auto ctrl) __attribute__((always_inline)) {
+    constexpr int C = decltype(ctrl)::value;
+    const uint32_t b = __builtin_bit_cast(uint32_t, v);
+    return __builtin_bit_cast(V, lane_move<C, 0xf>(b, b));
+  };
+  using std::integral_constant;
+  v = op(v, moved(integral_constant<int, 0xb1>()));    // neighbours, pairs, halves of eight, of sixteen
+  v = op(v, moved(integral_constant<int, 0x4e>()));
+  v = op(v, moved(integral_constant<int, 0x141>()));
+  v = op(v, moved(integral_constant<int, 0x140>()));
+  if constexpr (G >= 32) v = op(v, __shfl_xor(v, 16));
+  if constexpr (G >= 64) v = op(v, __shfl_xor(v, 32));
+  return v;
+}
+
+template <typename T, int G>
+__global__ __launch_bounds__(256) void logprobs_small_kernel(LogprobParams p) {
+  constexpr int kRows = 64 / G;
+  __shared__ __align__(16) uint32_t orders[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, id = lane % G;
+  const int64_t row = ((((int64_t)blockIdx.y << kGridShift) + blockIdx.x) * 4 + wave) * kRows + lane / G;
+  if (row >= p.rows) return;                           // (no barriers below)
+  const float ninf = -__builtin_inff();
+  const float x = id < p.V ? to_float(((const T*)p.x + row * p.xs)[id]) : ninf;
+  Ahead ahead;
+  ahead.load<T>(p, row, id);
+  const float m = row_reduce<G>(x, [](float a, float b) { return fmaxf(a, b); });
+  const float base = m == ninf ? 0.0f : m, d = x - base, e = __expf(d);
+  const float s = row_reduce<G>(e, [](float a, float b) { return a + b; });
+  const float t = row_reduce<G>(e * fmaxf(d, -1000.0f), [](float a, float b) { return a + b; });
+  const Scorer score(m, s, t);
+  score.template tokens<T>(p, row, id, G, ahead);
+  if (p.top == 0) return;
+  const uint32_t own = id < p.V ? order_of(x) : 0;
+  if (4 * p.top < p.V) {
+    // few: taken out one after the other, of equal ones the lowest (a lane's number is 0 once it was taken)
+    uint32_t left = own;
+    for (int j = 0; j < p.top; ++j) {
+      const uint32_t most = row_reduce<G>(left, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+      const uint64_t at = __ballot(left == most && id < p.V) >> (lane / G * G);
+      if (id == __ffsll((unsigned long long)at) - 1) {
+        score.alternative(p, row, j, (uint64_t)own << 32 | (uint32_t)~id);
+        left = 0;
+      }
+    }
+    return;
+  }
+  orders[wave][lane] = own;
+  sync<1>();
+  int rank = 0;
+#pragma unroll 2
+  for (int o = 0; o < p.V; o += 4) {                   // (lanes past the row hold 0)
+    const v4u c = *reinterpret_cast<const v4u*>(&orders[wave][lane / G * G + o]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) rank += c[k] > own || (c[k] == own && o + k < id);
+  }
+  if (rank < p.top && id < p.V) score.alternative(p, row, rank, (uint64_t)own << 32 | (uint32_t)~id);
+}
+
 // A workgroup joins the pieces of a row.
 constexpr int kJoinWaves = 4, kHeld = 16;              // keys that a thread holds
 template <typename T>
@@ -378,6 +407,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(LogprobParams p, 
   const int64_t row = ((int64_t)blockIdx.y << kGridShift) + blockIdx.x;
   if (row >= p.rows) return;
   const int tid = threadIdx.x, lane = tid & 63;
+  Ahead ahead;
+  ahead.load<T>(p, row, tid);
   const uint64_t* keys = c.best + row * c.n * p.top;
   const int n = c.n * p.top;
   uint64_t held[kHeld];
@@ -399,7 +430,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(LogprobParams p, 
   s = wave_sum(s);
   t = wave_sum(t);
   const Scorer score(m, s, t);
-  score.template tokens<T>(p, row, tid, 64 * W);
+  score.template tokens<T>(p, row, tid, 64 * W, ahead);
   if (p.top == 0) return;
   auto leave = [&](int j, uint64_t key) __attribute__((always_inline)) { score.alternative(p, row, j, key); };
   if (n > kHeld * 64 * W) {
@@ -434,9 +465,10 @@ Pieces pieces_of(int64_t rows, int V, int bytes) {
   Pieces c{};
   const int64_t all = (int64_t)V * bytes;
   int64_t n = (all + kWhole - 1) / kWhole;
-  // few long rows: pieces for the whole chip, of 8 KiB and more
+  // few long rows: pieces for the whole chip, of 8 KiB and more (a row that one workgroup can take is done before a second kernel
+  // would begin: 32000 float32 logits in 6.7 us, five alternatives with them, against 9.9 in 15 pieces)
   const int64_t want = 256 / rows, most = (all + 8191) / 8192;
-  if (want > n) n = want < most ? want : most > n ? most : n;
+  if (n > 1 && want > n) n = want < most ? want : most;
   const int per = 16 / bytes;
   c.len = (int)(((V + n - 1) / n + per - 1) / per * per);
   c.n = (int)((V + (int64_t)c.len - 1) / c.len);
@@ -471,6 +503,12 @@ hipError_t launch_logprobs(const LogprobParams& p, int x_type, void* workspace, 
       const GridShape g = grid_shape(waves == 1 ? (units + 3) / 4 : units);
       return launch_kernel(kernel, dim3(g.x, g.y), dim3(waves == 1 ? 256 : 64 * waves), 0, st, p, c);
     };
+    if (p.V <= 64) {
+      const int G = p.V <= 16 ? 16 : p.V <= 32 ? 32 : 64, rows = 4 * 64 / G;
+      const GridShape g = grid_shape((p.rows + rows - 1) / rows);
+      return launch_kernel(G == 16 ? logprobs_small_kernel<T, 16> : G == 32 ? logprobs_small_kernel<T, 32> : logprobs_small_kernel<T, 64>,
+                           dim3(g.x, g.y), dim3(256), 0, st, p);
+    }
     if (loads <= 64) e = launch(logprobs_kernel<T, 1, 1>, 1);
     else if (loads <= 256) e = launch(logprobs_kernel<T, 1, 4>, 1);
     else if (loads <= 512) e = launch(logprobs_kernel<T, 4, 2>, 4);

@@ -125,10 +125,10 @@ def test_logprob_workspace():
     for rows, V in ((1, 1 << 18), (3, 1 << 20), (1, (1 << 31) - 1)):
         need = Q.logprobs_workspace_bytes(rows, V, 20)
         if need:
-            assert logprobs(rows=rows, V=V, x=f(1 << 40), nbytes=need - 1) == WORKSPACE
-            assert logprobs(rows=rows, V=V, x=f(1 << 40), nbytes=need, work=None) == WORKSPACE
-            assert logprobs(rows=rows, V=V, x=f(1 << 40), nbytes=need, work=f(G.value + 64)) == WORKSPACE
-            assert logprobs(rows=rows, V=V, x=f(1 << 40), nbytes=need, work=D) == ALIAS
+            assert logprobs(rows=rows, V=V, x=f(1 << 40), top=20, nbytes=need - 1) == WORKSPACE
+            assert logprobs(rows=rows, V=V, x=f(1 << 40), top=20, nbytes=need, work=None) == WORKSPACE
+            assert logprobs(rows=rows, V=V, x=f(1 << 40), top=20, nbytes=need, work=f(G.value + 64)) == WORKSPACE
+            assert logprobs(rows=rows, V=V, x=f(1 << 40), top=20, nbytes=need, work=D) == ALIAS
 
 
 def test_binding_holds_tensors_against_the_call():

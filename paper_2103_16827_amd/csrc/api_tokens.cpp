@@ -116,6 +116,9 @@ qasr_status qasr_linear_int8_dynamic(const qasr_linear_desc* desc, const void* x
   if (overlaps(workspace, nws, x, nx) || overlaps(workspace, nws, w, nw) || overlaps(workspace, nws, w_scale, nn) ||
       overlaps(workspace, nws, bias, nn) || overlaps(workspace, nws, y, ny))
     return QASR_ERR_ALIAS;
+  qasr::LinearParams p = linear_params(d, nullptr, nullptr, w, w_scale, bias, y);
+  p.xf = x;
+  if (qasr::linear_takes_floats(p, x_type)) return hip_status(qasr::launch_linear_floats(p, x_type, (hipStream_t)stream));
   const int64_t pitch = round16(d.K);
   int8_t* codes = (int8_t*)workspace;
   float* scale = (float*)(codes + round256((size_t)d.M * (size_t)pitch));

@@ -142,8 +142,12 @@ struct LinearParams {
   const int32_t* index;   // row of x of each row of y, or null
   int32_t E, x_rows;
   int64_t wes;            // elements between matrices
+  const void* xf;         // launch_linear_floats: the tokens (xs then is theirs)
 };
 hipError_t launch_linear(const LinearParams& p, hipStream_t st);
+// One matrix on float tokens, quantised row by row in the same launch; whether it takes them.
+bool linear_takes_floats(const LinearParams& p, int x_type);
+hipError_t launch_linear_floats(const LinearParams& p, int x_type, hipStream_t st);
 
 // One call of qasr_token_logprobs.
 struct LogprobParams {

@@ -13,7 +13,9 @@
 // linear_tile (more): tiles of BM x BN through a ring in LDS that the waves share, a barrier per step.
 #include "floats.hpp"
 #include "kernels.hpp"
+#include "lanes.hpp"
 #include "launch_shape.hpp"
+#include "quantize_row.hpp"
 #include "vmem.hpp"
 
 #include <algorithm>
@@ -170,11 +172,19 @@ __device__ __forceinline__ float channel_bias(const LinearParams& L, const Tile&
 
 // ---- few tokens
 
-// W waves; wave w takes the steps w, w + W, ...; DIRECT: rows 16-byte aligned, K a multiple of 16
-template <int MT, int NT, int W, int S, bool DIRECT, typename T>
+// Elements of x that linear_few quantises by itself: they are in registers in between.
+constexpr int kFloats = 8192;
+
+// W waves; wave w takes the steps w, w + W, ...; DIRECT: rows 16-byte aligned, K a multiple of 16.
+// X: int8_t, or the type of float tokens, up to 16 of them and kFloats elements, that every workgroup quantises for itself while its
+// weights are on their way (a launch less, which for one token is half of the time); their rows 16-byte aligned.
+template <int MT, int NT, int W, int S, bool DIRECT, typename X, typename T>
 __global__ __launch_bounds__(64 * W) void linear_few_kernel(LinearParams L, Order o) {
+  constexpr bool FLOATS = !__is_same(X, int8_t);
+  static_assert(!FLOATS || (DIRECT && MT == 1), "floats: one product of tokens");
   constexpr int STEP = 128, P = products_of<T>(NT);
-  constexpr int BM = 16 * MT, BN = 16 * NT, kLoads = (BM + BN) / 8, kStage = (BM + BN) * STEP;
+  constexpr int BM = 16 * MT, BN = 16 * NT, TOKENS = FLOATS ? 0 : BM;          // rows of tokens in a stage
+  constexpr int kLoads = (TOKENS + BN) / 8, kStage = (TOKENS + BN) * STEP;
   static_assert(S * kStage >= MT * NT * 1024, "a wave's partial sums go where its ring was");
   extern __shared__ __align__(1024) unsigned char lds[];
   Tile t;
@@ -182,21 +192,24 @@ __global__ __launch_bounds__(64 * W) void linear_few_kernel(LinearParams L, Orde
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   unsigned char* ring = lds + wave * (S * kStage);
 
-  const int steps = (L.K + STEP - 1) / STEP;
+  const int steps = (L.K + STEP - 1) / STEP, rows = t.hi - t.lo;
   const int mine = wave < steps ? (steps - wave + W - 1) / W : 0;
   const int8_t* row[kLoads];
   int chunk[kLoads];
+  bool brings[kLoads];             // rows that there are, and a row of every load: the waits count loads
 #pragma unroll
   for (int j = 0; j < kLoads; ++j) {
     const int i = 8 * j + (lane >> 3);
-    if (8 * j < BM) {
-      const int xr = x_row(L, min(t.lo + i, t.hi - 1));
+    if (8 * j < TOKENS) {
+      const int xr = x_row(L, t.lo + min(i, rows - 1));
       row[j] = L.x + (int64_t)max(xr, 0) * L.xs;
       chunk[j] = (lane & 7) ^ swizzle<STEP>(i & 15);
+      brings[j] = i < rows || i % 8 == 0;
     } else {
-      const int n = i - BM;
+      const int n = i - TOKENS;
       row[j] = L.w + t.e * L.wes + (int64_t)min(t.n0 + n, L.N - 1) * L.ws;
       chunk[j] = (lane & 7) ^ swizzle<STEP>(row_of<P>(n));
+      brings[j] = true;
     }
   }
 
@@ -206,7 +219,7 @@ __global__ __launch_bounds__(64 * W) void linear_few_kernel(LinearParams L, Orde
     Item it;
     it.m = t.lo + 16 * (i / NT) + r;
     it.n = t.n0 + channel_of<P>(i % NT, 4 * g);
-    it.sx = token_scale(L, min(it.m, t.hi - 1));
+    it.sx = FLOATS ? 0.0f : token_scale(L, min(it.m, t.hi - 1));
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       it.ws[c] = channel_scale(L, t, it.n + c);
@@ -222,15 +235,22 @@ __global__ __launch_bounds__(64 * W) void linear_few_kernel(LinearParams L, Orde
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = (v4i){0, 0, 0, 0};
 
-  auto products = [&](const unsigned char* stage) __attribute__((always_inline)) {
+  // FLOATS: the tokens' codes, rows of `pitch` bytes whose chunk c of 128 bytes is at c ^ (row & 7), and their scales
+  unsigned char* codes = lds + W * S * kStage;
+  const int pitch = steps * STEP, own = min(r, rows - 1);
+  float* code_scale = (float*)(codes + rows * pitch);
+  auto products = [&](const unsigned char* stage, int k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int at = 16 * ((4 * h + g) ^ swizzle<STEP>(r));
       v4i a[MT], b[NT];
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) a[mt] = *(const v4i*)(stage + (16 * mt + r) * STEP + at);
+      for (int mt = 0; mt < MT; ++mt) {
+        if constexpr (FLOATS) a[mt] = *(const v4i*)(codes + own * pitch + k0 + 16 * ((4 * h + g) ^ (own & 7)));
+        else a[mt] = *(const v4i*)(stage + (16 * mt + r) * STEP + at);
+      }
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) b[nt] = *(const v4i*)(stage + (BM + channel_of<P>(nt, r)) * STEP + at);
+      for (int nt = 0; nt < NT; ++nt) b[nt] = *(const v4i*)(stage + (TOKENS + channel_of<P>(nt, r)) * STEP + at);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -246,14 +266,68 @@ __global__ __launch_bounds__(64 * W) void linear_few_kernel(LinearParams L, Orde
       for (int j = 0; j < kLoads; ++j) {
         const int k = k0 + 16 * chunk[j];
         const void* p = k < L.K ? (const void*)(row[j] + k) : (const void*)kZeros;
-        direct_load16(p, stage + 1024 * j);
+        if (brings[j]) direct_load16(p, stage + 1024 * j);
       }
     };
     for (int i = 0; i < min(S, mine); ++i) ask(i);
+    if constexpr (FLOATS) {
+      constexpr int N = kPer<X>, R = kFloats / N / (64 * W);
+      const int per = L.K / N, all = rows * per;               // pieces of 16 bytes
+      uint32_t* most = (uint32_t*)(code_scale + 16);
+      if (threadIdx.x < 16) most[threadIdx.x] = 0;
+      v4u raw[R];
+      int of[R];
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        const int c = threadIdx.x + j * 64 * W;
+        of[j] = c / per;
+        raw[j] = (v4u){0, 0, 0, 0};
+        if (c < all) raw[j] = *reinterpret_cast<const v4u*>((const X*)L.xf + (int64_t)(t.lo + of[j]) * L.xs + (c - of[j] * per) * N);
+      }
+      // zeros behind the codes, up to a whole step
+      const int pad = (pitch - L.K) / 16;
+      for (int j = threadIdx.x; j < rows * pad; j += 64 * W) {
+        const int m = j / pad, c = L.K / 16 + (j - m * pad);
+        *(v4i*)(codes + m * pitch + 16 * (c ^ (m & 7))) = (v4i){0, 0, 0, 0};
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        if (threadIdx.x - lane + j * 64 * W >= all) break;       // (the whole wave)
+        uint32_t a = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t word = sign_off<X>(raw[j][k]);
+          if constexpr (sizeof(X) == 4) a = max(a, word < kInf<X> ? word : 0u);
+          else a = max(a, max((word & 0xffffu) < kInf<X> ? word & 0xffffu : 0u, word >> 16 < kInf<X> ? word >> 16 : 0u));
+        }
+        // one update for a wave that is in one row
+        if (__builtin_amdgcn_readfirstlane(of[j]) == __builtin_amdgcn_readlane(of[j], 63)) {
+          a = wave_max(a);
+          if (lane == 0) atomicMax(&most[of[j]], a);
+        } else if (of[j] < rows) {
+          atomicMax(&most[of[j]], a);
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        const int c = threadIdx.x + j * 64 * W, k = (c - of[j] * per) * N, m = of[j];
+        if (c >= all) break;
+        const float S_m = scale_of(magnitude<X>(most[m]));
+        if (k == 0) code_scale[m] = S_m;
+#pragma unroll
+        for (int w = 0; w < N / 4; ++w)
+          *(uint32_t*)(codes + m * pitch + 16 * ((k >> 4) ^ (m & 7)) + (k & 15) + 4 * w) =
+              codes_of(element<X>(raw[j], 4 * w), element<X>(raw[j], 4 * w + 1), element<X>(raw[j], 4 * w + 2), element<X>(raw[j], 4 * w + 3), S_m);
+      }
+      __syncthreads();
+      mine_at_end.sx = code_scale[own];
+    }
     for (int i = 0; i < mine; ++i) {
       if (i + S <= mine) wait_vm<(S - 1) * kLoads>();
       else wait_vm_dyn((mine - 1 - i) * kLoads);
-      products(ring + (i % S) * kStage);
+      products(ring + (i % S) * kStage, (wave + i * W) * STEP);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the slot has been read
       if (i + S < mine) ask(i + S);
     }
@@ -270,7 +344,7 @@ __global__ __launch_bounds__(64 * W) void linear_few_kernel(LinearParams L, Orde
       for (int j = 0; j < kLoads; ++j) *(v4i*)(ring + 1024 * j + 16 * lane) = next[j];
       if (i + 1 < mine) fetch(i + 1);
       __builtin_amdgcn_wave_barrier();
-      products(ring);
+      products(ring, 0);
       __builtin_amdgcn_wave_barrier();
     }
   }
@@ -609,15 +683,16 @@ Order order_of(const LinearParams& p, int BM, int BN) { return Order{(p.N + BN -
 
 GridShape grid_of(const Order& o) { return grid_shape(((int64_t)o.mt * o.nt + 7) / 8 * 8); }
 
-template <int MT, int NT, int W, int S, bool DIRECT, typename T>
+template <int MT, int NT, int W, int S, bool DIRECT, typename X, typename T>
 hipError_t launch_few(const LinearParams& p, hipStream_t st) {
   const Order o = order_of(p, 16 * MT, 16 * NT);
   const GridShape g = grid_of(o);
-  constexpr int bytes = W * S * 16 * (MT + NT) * 128;
+  constexpr bool floats = !__is_same(X, int8_t);
+  const int bytes = W * S * 16 * ((floats ? 0 : MT) + NT) * 128 + (floats ? p.M * ((p.K + 127) / 128 * 128) + 128 : 0);
   static std::atomic<uint64_t> done;
-  const hipError_t e = ensure_max_dynamic_lds((const void*)linear_few_kernel<MT, NT, W, S, DIRECT, T>, done);
+  const hipError_t e = ensure_max_dynamic_lds((const void*)linear_few_kernel<MT, NT, W, S, DIRECT, X, T>, done);
   if (e != hipSuccess) return e;
-  return launch_kernel(linear_few_kernel<MT, NT, W, S, DIRECT, T>, dim3(g.x, g.y), dim3(64 * W), bytes, st, p, o);
+  return launch_kernel(linear_few_kernel<MT, NT, W, S, DIRECT, X, T>, dim3(g.x, g.y), dim3(64 * W), bytes, st, p, o);
 }
 
 template <int MT, int NT, int WM, int WN, int S, typename T>
@@ -693,15 +768,15 @@ template <typename T>
 hipError_t launch_typed(const LinearParams& p, hipStream_t st) {
   if (!direct_ok(p)) {
     const double rows = p.offsets ? (double)p.M / p.E : p.M;
-    if (rows <= 16) return launch_few<1, 1, 8, 1, false, T>(p, st);
-    if (rows <= 64) return launch_few<4, 2, 4, 1, false, T>(p, st);
+    if (rows <= 16) return launch_few<1, 1, 8, 1, false, int8_t, T>(p, st);
+    if (rows <= 64) return launch_few<4, 2, 4, 1, false, int8_t, T>(p, st);
     return launch_rows<4, 4, 2, 2, T>(p, st);
   }
   switch (fastest_form(p)) {
-    case 0: return launch_few<1, 1, 8, 2, true, T>(p, st);
-    case 1: return launch_few<2, 2, 4, 2, true, T>(p, st);
-    case 2: return launch_few<2, 4, 4, 2, true, T>(p, st);
-    case 3: return launch_few<4, 4, 4, 2, true, T>(p, st);
+    case 0: return launch_few<1, 1, 8, 2, true, int8_t, T>(p, st);
+    case 1: return launch_few<2, 2, 4, 2, true, int8_t, T>(p, st);
+    case 2: return launch_few<2, 4, 4, 2, true, int8_t, T>(p, st);
+    case 3: return launch_few<4, 4, 4, 2, true, int8_t, T>(p, st);
     case 4: return launch_tile<2, 4, 2, 2, 3, T>(p, st);
     case 5: return launch_tile<4, 4, 2, 2, 4, T>(p, st);
     case 6: return launch_tile<4, 4, 2, 4, 3, T>(p, st);
@@ -710,6 +785,23 @@ hipError_t launch_typed(const LinearParams& p, hipStream_t st) {
 }
 
 }  // namespace
+
+// Few enough floats for every workgroup to quantise them: with kFloats over all rounds of workgroups on the chip it takes
+// less than the launch that it saves.
+bool linear_takes_floats(const LinearParams& p, int x_type) {
+  const int64_t size = x_type == 0 ? 4 : 2, all = (int64_t)p.M * p.K;
+  LinearParams codes = p;                // as if tokens were codes on a boundary: the weights are what is asked about
+  codes.x = nullptr;
+  codes.xs = (p.K + 15) / 16 * 16;
+  return p.M <= 16 && all * ((p.N + 8191) / 8192) <= kFloats && direct_ok(codes) && (uintptr_t)p.xf % 16 == 0 &&
+         (p.M == 1 || p.xs * size % 16 == 0);
+}
+
+hipError_t launch_linear_floats(const LinearParams& p, int x_type, hipStream_t st) {
+  return with_type(x_type, [&](auto x) {
+    return with_type(p.y_type, [&](auto t) { return launch_few<1, 1, 8, 2, true, decltype(x), decltype(t)>(p, st); });
+  });
+}
 
 hipError_t launch_linear(const LinearParams& p, hipStream_t st) {
   return with_type(p.y_type, [&](auto t) { return launch_typed<decltype(t)>(p, st); });

@@ -8,55 +8,10 @@
 #include "kernels.hpp"
 #include "lanes.hpp"
 #include "launch_shape.hpp"
+#include "quantize_row.hpp"
 
 namespace qasr {
 namespace {
-
-typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-typedef unsigned short v2us __attribute__((ext_vector_type(2)));
-
-template <typename T>
-constexpr int kPer = 16 / (int)sizeof(T);              // elements per 16 bytes
-
-// Magnitudes as unsigned numbers in the type's own bits: what is kInf or above is no finite number.
-template <typename T>
-constexpr uint32_t kInf = sizeof(T) == 4 ? 0x7f800000u : __is_same(T, bf16) ? 0x7f80u : 0x7c00u;
-template <typename T>
-__device__ __forceinline__ uint32_t bits_of(T v) {
-  if constexpr (sizeof(T) == 4) return __builtin_bit_cast(uint32_t, v);
-  else return __builtin_bit_cast(uint16_t, v);
-}
-template <typename T>
-__device__ __forceinline__ float magnitude(uint32_t bits) {
-  if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, bits);
-  else return to_float(__builtin_bit_cast(T, (uint16_t)bits));
-}
-template <typename T>
-__device__ __forceinline__ uint32_t sign_off(uint32_t word) { return word & (sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu); }
-template <typename T>
-__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {        // of a word's numbers
-  if constexpr (sizeof(T) == 4) return a > b ? a : b;
-  else return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2us, a), __builtin_bit_cast(v2us, b)));
-}
-template <typename T>
-__device__ __forceinline__ uint32_t largest_of(uint32_t word) {
-  if constexpr (sizeof(T) == 4) return word;
-  else return (word & 0xffffu) > word >> 16 ? word & 0xffffu : word >> 16;
-}
-template <typename T>
-__device__ __forceinline__ float element(const v4u& v, int e) {
-  const uint32_t word = v[sizeof(T) == 4 ? e : e >> 1];
-  if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, word);
-  else return to_float(__builtin_bit_cast(T, (uint16_t)(e & 1 ? word >> 16 : word)));
-}
-
-__device__ __forceinline__ float scale_of(float a) { return a > 0.0f ? fmaxf(__fdiv_rn(a, 127.0f), 0x1p-126f) : 1.0f; }
-// (the conversion saturates, and makes 0 of a NaN: what is clipped here is what the definition clips before it rounds)
-__device__ __forceinline__ int32_t code_of(float v, float S) {
-  int32_t q;
-  asm("v_cvt_i32_f32 %0, %1" : "=v"(q) : "v"(rintf(__fdiv_rn(v, S))));
-  return min(127, max(-127, q));
-}
 
 // W waves a row, R loads of 16 bytes a lane from a 16-byte boundary on; what is before and behind them, an element for
 // each of the first threads.  W == 1: four rows a workgroup, a wave each.
@@ -121,12 +76,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void quantize_tokens_kernel(
     if (i * 64 * W + tid < loads) {
       struct __attribute__((packed)) { uint32_t word[N / 4]; } out;
 #pragma unroll
-      for (int w = 0; w < N / 4; ++w) {
-        int32_t c[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) c[k] = code_of(element<T>(raw[i], 4 * w + k), S);
-        out.word[w] = __builtin_amdgcn_perm((uint32_t)c[1], (uint32_t)c[0], 0x0c0c0400u) | __builtin_amdgcn_perm((uint32_t)c[3], (uint32_t)c[2], 0x04000c0cu);
-      }
+      for (int w = 0; w < N / 4; ++w)
+        out.word[w] = codes_of(element<T>(raw[i], 4 * w), element<T>(raw[i], 4 * w + 1), element<T>(raw[i], 4 * w + 2), element<T>(raw[i], 4 * w + 3), S);
       *reinterpret_cast<decltype(out)*>(to + head + (i * 64 * W + tid) * N) = out;
     }
   if (rest < K) to[rest] = (int8_t)code_of(to_float(last), S);

@@ -13,8 +13,9 @@ template <int CTRL, int ROWS>
 __device__ __forceinline__ uint32_t lane_move(uint32_t keep, uint32_t v) {
   return (uint32_t)__builtin_amdgcn_update_dpp((int)keep, (int)v, CTRL, ROWS, 0xf, false);
 }
+// every lane's v with those of the lanes before it
 template <typename V, typename Op>
-__device__ __forceinline__ V wave_reduce(V v, V none, Op op) {
+__device__ __forceinline__ V wave_scan(V v, V none, Op op) {
   auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
     constexpr int C = decltype(ctrl)::value, R = decltype(rows)::value;
     if constexpr (sizeof(V) == 8) {
@@ -32,6 +33,11 @@ __device__ __forceinline__ V wave_reduce(V v, V none, Op op) {
   step(integral_constant<int, 0x118>(), integral_constant<int, 0xf>());
   step(integral_constant<int, 0x142>(), integral_constant<int, 0xa>());      // the last of a row to the row after it (rows 1 and 3)
   step(integral_constant<int, 0x143>(), integral_constant<int, 0xc>());      // the last of the second row to the third and fourth
+  return v;
+}
+template <typename V, typename Op>
+__device__ __forceinline__ V wave_reduce(V v, V none, Op op) {
+  v = wave_scan(v, none, op);
   if constexpr (sizeof(V) == 8) {
     const uint64_t b = __builtin_bit_cast(uint64_t, v);
     return __builtin_bit_cast(V, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), 63) << 32 |

@@ -67,40 +67,36 @@ __device__ __forceinline__ uint32_t first_unit() { return (blockIdx.y << kGridSh
 template <int BM>
 __device__ __forceinline__ bool group_tile(const LinearParams& L, const Order& o, uint32_t unit, int BN, Tile& t) {
   const int lane = threadIdx.x & 63;
-  int64_t total = 0;
-  for (int e0 = 0; e0 < L.E; e0 += 64) {
+  int a, b;                                 // the lane's group among the 64 from e0 on, and its tiles
+  auto upto = [&](int e0, int& n) __attribute__((always_inline)) {
     const int e = min(e0 + lane, L.E - 1);
-    const int a = offset_at(L, e), b = offset_at(L, e + 1);
-    int n = e0 + lane < L.E && b > a ? (b - a + BM - 1) / BM : 0;
-    for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
-    total += n;
-  }
+    a = offset_at(L, e);
+    b = offset_at(L, e + 1);
+    n = e0 + lane < L.E && b > a ? (b - a + BM - 1) / BM : 0;
+    return wave_scan(n, 0, [](int x, int y) { return x + y; });
+  };
+  int n, before = upto(0, n), total = __builtin_amdgcn_readlane(before, 63);
+  for (int e0 = 64; e0 < L.E && total < o.mt; e0 += 64) total += __builtin_amdgcn_readlane(upto(e0, n), 63);
+  if (L.E > 64) before = upto(0, n);
   // (more than o.mt only where offsets decrease)
-  const int tiles = __builtin_amdgcn_readfirstlane((int)min(total, (int64_t)o.mt));
-  const int u = xcd_order(unit, (uint32_t)tiles * o.nt);
+  const int u = xcd_order(unit, (uint32_t)min(total, o.mt) * o.nt);
   if (u < 0) return false;
   int left = u / o.nt;
   t.n0 = (u - left * o.nt) * BN;
-  for (int e0 = 0; e0 < L.E; e0 += 64) {
-    const int e = min(e0 + lane, L.E - 1);
-    const int a = offset_at(L, e), b = offset_at(L, e + 1);
-    const int n = e0 + lane < L.E && b > a ? (b - a + BM - 1) / BM : 0;
-    int upto = n;                           // tiles of this group and of those before it
-    for (int d = 1; d < 64; d <<= 1) {
-      const int v = __shfl_up(upto, d);
-      upto += lane >= d ? v : 0;
-    }
-    const int all = __builtin_amdgcn_readlane(upto, 63);
+  for (int e0 = 0;;) {
+    const int all = __builtin_amdgcn_readlane(before, 63);
     if (left < all) {
-      const int src = __popcll(__ballot(upto <= left));
+      const int src = __popcll(__ballot(before <= left));
       t.e = e0 + src;
-      t.lo = __shfl(a, src) + (left - __shfl(upto - n, src)) * BM;
-      t.hi = min(__shfl(b, src), t.lo + BM);
+      t.lo = __builtin_amdgcn_readlane(a, src) + (left - __builtin_amdgcn_readlane(before - n, src)) * BM;
+      t.hi = min(__builtin_amdgcn_readlane(b, src), t.lo + BM);
       return true;
     }
     left -= all;
+    e0 += 64;
+    if (e0 >= L.E) return false;
+    before = upto(e0, n);
   }
-  return false;
 }
 
 // the same for one matrix: `along` tiles of rows by all tiles of channels, the rows going first
@@ -120,11 +116,7 @@ __device__ __forceinline__ bool plain_tile(const LinearParams& L, const Order& o
 template <int BM>
 __device__ __forceinline__ bool find_tile(const LinearParams& L, const Order& o, uint32_t unit, int BN, Tile& t) {
   if (!L.offsets) return plain_tile<BM>(L, o, unit, BN, t);
-  const bool found = group_tile<BM>(L, o, unit, BN, t);
-  t.e = __builtin_amdgcn_readfirstlane(t.e);
-  t.lo = __builtin_amdgcn_readfirstlane(t.lo);
-  t.hi = __builtin_amdgcn_readfirstlane(t.hi);
-  return found;
+  return group_tile<BM>(L, o, unit, BN, t);
 }
 
 // row of x that row m of y reads, -1 for one that is not there
@@ -724,41 +716,43 @@ bool direct_ok(const LinearParams& p) {
   return p.ws < most / 256 && (p.index ? p.xs < most / p.x_rows : p.xs < most / 256);
 }
 
-// What a form of the kernels takes for one tile on a compute unit, in us: `end` for its beginning and end, `alone` for a step of 128
-// codes with nothing else on the chip, `busy` with a tile on every unit.  Fitted to 22 shapes of 1 to 4096 tokens on weights that
-// are not in a cache; next to the fastest form of each shape, what the rule takes cost 0 to 10 % more.
-struct Form { int BM, BN, per_unit; double end, alone, busy; };
+// What a form of the kernels takes for one tile on a compute unit, in us: `end` for its beginning and end, `group` more of that
+// where a tile's rows have to be found first, and for a step of 128 codes `alone` with nothing else on the chip, `busy` with
+// a tile on every unit.  Fitted to 10 forms x 36 shapes of 1 to 16384 rows, 10 of them in groups, on weights that no cache held (rms 6 to 16 %
+// by form); next to the fastest form of each shape, the one that the rule takes cost nothing in 32 of them and at most 10 %.
+struct Form { int BM, BN, per_unit; double end, group, alone, busy; };
 constexpr Form kForms[] = {
-    {16, 16, 2, 0.15, 0.09, 0.0535},   // linear_few, from here
-    {32, 32, 2, 0.3, 0.12, 0.106},
-    {32, 64, 1, 0.4, 0.17, 0.2},
-    {64, 64, 1, 0.5, 0.24, 0.35},
-    {64, 128, 2, 2.0, 0.29, 0.375},    // linear_tile, from here
-    {128, 128, 1, 2.0, 0.40, 0.65},
-    {128, 256, 1, 3.0, 0.57, 1.0},
-    {256, 256, 1, 5.5, 1.1, 1.7},
+    {16, 16, 5, 0.29, 1.5, 0.085, 0.039},      // linear_few, from here
+    {16, 32, 3, 0.44, 1.6, 0.103, 0.062},
+    {16, 64, 4, 0.48, 2.2, 0.212, 0.109},
+    {32, 32, 2, 0.88, 1.1, 0.128, 0.088},
+    {32, 64, 1, 2.2, 1.2, 0.132, 0.185},
+    {64, 64, 1, 3.8, 1.1, 0.210, 0.265},
+    {64, 128, 2, 1.2, 1.4, 0.306, 0.362},      // linear_tile, from here
+    {128, 128, 1, 2.8, 1.0, 0.375, 0.617},
+    {128, 256, 1, 4.0, 0.1, 0.525, 0.993},
+    {256, 256, 1, 4.4, 0.0, 1.033, 1.821},
 };
 constexpr int kFormCount = sizeof(kForms) / sizeof(kForms[0]);
-
-// tiles of BM rows that a launch will have: for groups, of which only the device knows the sizes, as if rows fell on them by chance
-double expected_row_tiles(const LinearParams& p, int BM) {
-  if (!p.offsets) return (double)row_tiles(p, BM);
-  const double busy = p.E * (1.0 - std::pow(1.0 - 1.0 / p.E, (double)p.M)), rows = p.M / busy;
-  return busy * (rows <= BM / 2 ? 1.0 : rows / BM + 0.5);
-}
+constexpr double kBytesPerUs = 5.3e6;           // of memory
 
 int fastest_form(const LinearParams& p) {
   const double steps = (p.K + 127) / 128, units = compute_units();
+  // groups, of which only the device knows the sizes: as if rows fell on them by chance
+  const double groups = p.offsets ? p.E * (1.0 - std::pow(1.0 - 1.0 / p.E, (double)p.M)) : 1.0, rows = p.M / groups;
+  const double memory = (groups * p.N * p.K + (double)p.M * (p.K + 2.0 * p.N)) / kBytesPerUs;
   int best = 0;
   double least = 0;
   for (int i = 0; i < kFormCount; ++i) {
     const Form& f = kForms[i];
-    const double tiles = expected_row_tiles(p, f.BM) * ((p.N + f.BN - 1) / f.BN), load = tiles / units;
-    const double us = std::max(std::ceil(load / f.per_unit) * (f.end + steps * f.alone),
-                               (load > 1 ? std::ceil(load) : std::sqrt(std::sqrt(load))) * (f.end + steps * f.busy));
-    if (i == 0 || us < least) {
+    const double in_group = !p.offsets ? std::ceil(rows / f.BM) : rows <= f.BM / 2 ? 1.0 : rows / f.BM + 0.5;
+    const double load = groups * in_group * ((p.N + f.BN - 1) / f.BN) / units, group = p.offsets ? f.group : 0.0;
+    const double us = std::max(std::ceil(load / f.per_unit) * (f.end + group + steps * f.alone),
+                               (load > 1 ? std::ceil(load) : std::sqrt(std::sqrt(load))) * (f.end + group / f.per_unit + steps * f.busy));
+    const double cubes = us * us * us + memory * memory * memory;      // (the longer of the two, and a little of the other)
+    if (i == 0 || cubes < least) {
       best = i;
-      least = us;
+      least = cubes;
     }
   }
   return best;
@@ -773,13 +767,15 @@ hipError_t launch_typed(const LinearParams& p, hipStream_t st) {
     return launch_rows<4, 4, 2, 2, T>(p, st);
   }
   switch (fastest_form(p)) {
-    case 0: return launch_few<1, 1, 8, 2, true, int8_t, T>(p, st);
-    case 1: return launch_few<2, 2, 4, 2, true, int8_t, T>(p, st);
-    case 2: return launch_few<2, 4, 4, 2, true, int8_t, T>(p, st);
-    case 3: return launch_few<4, 4, 4, 2, true, int8_t, T>(p, st);
-    case 4: return launch_tile<2, 4, 2, 2, 3, T>(p, st);
-    case 5: return launch_tile<4, 4, 2, 2, 4, T>(p, st);
-    case 6: return launch_tile<4, 4, 2, 4, 3, T>(p, st);
+    case 0: return launch_few<1, 1, 4, 2, true, int8_t, T>(p, st);
+    case 1: return launch_few<1, 2, 4, 2, true, int8_t, T>(p, st);
+    case 2: return launch_few<1, 4, 4, 1, true, int8_t, T>(p, st);
+    case 3: return launch_few<2, 2, 4, 2, true, int8_t, T>(p, st);
+    case 4: return launch_few<2, 4, 4, 2, true, int8_t, T>(p, st);
+    case 5: return launch_few<4, 4, 4, 2, true, int8_t, T>(p, st);
+    case 6: return launch_tile<2, 4, 2, 2, 3, T>(p, st);
+    case 7: return launch_tile<4, 4, 2, 2, 4, T>(p, st);
+    case 8: return launch_tile<4, 4, 2, 4, 3, T>(p, st);
     default: return launch_tile<8, 4, 2, 4, 2, T>(p, st);
   }
 }

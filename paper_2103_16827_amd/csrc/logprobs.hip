@@ -22,7 +22,6 @@ namespace {
 
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
-constexpr int kMaxTop = 64;
 constexpr int kRoom = 512;          // candidates that are ranked at once
 
 // order of a float as an unsigned number; zeros of either sign are equal

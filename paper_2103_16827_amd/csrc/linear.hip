@@ -30,11 +30,25 @@ constexpr int kLdsBytes = 160 * 1024;
 
 __device__ __align__(16) const uint8_t kZeros[16] = {};   // what stands for codes past the end of a row
 
-// bytes [k, k + 16) of a row of K bytes, zeros past its end; any alignment
+// Bytes [k, k + 16) of a row of K bytes, zeros past its end; any alignment.  A row's last bytes are loaded with those before
+// them and shifted down (byte by byte they would be a chain of up to 15 round trips to memory).
 __device__ __forceinline__ v4i row_chunk(const int8_t* row, int k, int K) {
   if (k + 16 <= K) return *reinterpret_cast<const unaligned_chunk16*>(row + k);
   v4i v = (v4i){0, 0, 0, 0};
-  for (int i = 0; k + i < K; ++i) v[i >> 2] |= (int)((uint32_t)(uint8_t)row[k + i] << (8 * (i & 3)));
+  if (k >= K) return v;
+  if (K < 16) {
+    for (int i = 0; k + i < K; ++i) v[i >> 2] |= (int)((uint32_t)(uint8_t)row[k + i] << (8 * (i & 3)));
+    return v;
+  }
+  const v4i all = *reinterpret_cast<const unaligned_chunk16*>(row + K - 16);
+  const int by = k + 16 - K, words = by >> 2;              // 1 .. 15 bytes
+  uint32_t w[5];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] = (uint32_t)(words == 0 ? all[i] : words == 1 ? (i < 3 ? all[(i + 1) & 3] : 0) : words == 2 ? (i < 2 ? all[(i + 2) & 3] : 0) : (i < 1 ? all[3] : 0));
+  w[4] = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (int)__builtin_amdgcn_alignbyte(w[i + 1], w[i], by & 3);
   return v;
 }
 
@@ -632,34 +646,46 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_rows_kernel(LinearParams 
   }
   Scales<BM, BN, 64 * W> sc;
   sc.load(L, t);
-  v4i next[kLoads];
-  auto fetch = [&](int k) __attribute__((always_inline)) {
+  // step k's rows are asked for two steps before their products, into registers by turns
+  v4i next[2][kLoads];
+  auto fetch = [&](int k, v4i (&to)[kLoads]) __attribute__((always_inline)) {
+    if ((k + 1) * STEP <= L.K) {
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) next[j] = row_chunk(row[j], k * STEP + 16 * (j < kTokenLoads ? token_chunk : channel_chunk), L.K);
+      for (int j = 0; j < kLoads; ++j)
+        to[j] = *reinterpret_cast<const unaligned_chunk16*>(row[j] + k * STEP + 16 * (j < kTokenLoads ? token_chunk : channel_chunk));
+    } else if (k < steps) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) to[j] = row_chunk(row[j], k * STEP + 16 * (j < kTokenLoads ? token_chunk : channel_chunk), L.K);
+    }
   };
-  auto put = [&](unsigned char* stage) __attribute__((always_inline)) {
+  auto put = [&](unsigned char* stage, const v4i (&from)[kLoads]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) *(v4i*)(stage + 1024 * (j * W + wave) + 16 * lane) = next[j];
+    for (int j = 0; j < kLoads; ++j) *(v4i*)(stage + 1024 * (j * W + wave) + 16 * lane) = from[j];
   };
   Sums<MT, NT> acc;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = (v4i){0, 0, 0, 0};
-  fetch(0);
-  put(lds);
-  sc.put(scales);
-  __syncthreads();
-  for (int k = 0; k < steps; ++k) {
+  auto step = [&](int k, v4i (&free)[kLoads], const v4i (&ready)[kLoads]) __attribute__((always_inline)) {
     const unsigned char* stage = lds + (k & 1) * kStage;
-    if (k + 1 < steps) fetch(k + 1);
+    fetch(k + 2, free);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int at = 16 * ((4 * h + g) ^ swizzle<STEP>(r));
       products_of_half<MT, NT, P, STEP>(acc, stage + (16 * MT * wm + r) * STEP + at, stage + (BM + 16 * NT * wn + channel_of<P>(0, r)) * STEP + at);
     }
-    if (k + 1 < steps) put(lds + ((k + 1) & 1) * kStage);
+    if (k + 1 < steps) put(lds + ((k + 1) & 1) * kStage, ready);
     __syncthreads();
+  };
+  fetch(0, next[0]);
+  fetch(1, next[1]);
+  put(lds, next[0]);
+  sc.put(scales);
+  __syncthreads();
+  for (int k = 0; k < steps; k += 2) {
+    step(k, next[0], next[1]);
+    if (k + 1 < steps) step(k + 1, next[1], next[0]);
   }
   store_tile<MT, NT, BM, BN, 2 * kStage / W, T>(L, t, scales, lds + 2 * kStage / W * wave, 16 * MT * wm, 16 * NT * wn, acc);
 }
@@ -733,18 +759,25 @@ constexpr Form kForms[] = {
     {128, 256, 1, 4.0, 0.1, 0.525, 0.993},
     {256, 256, 1, 4.4, 0.0, 1.033, 1.821},
 };
-constexpr int kFormCount = sizeof(kForms) / sizeof(kForms[0]);
+// ... where rows begin anywhere or end inside a chunk (14 shapes, of which the rule takes the fastest form but for 4 to 9 % in three)
+constexpr Form kRowForms[] = {
+    {16, 16, 4, 0.3, 2.0, 0.15, 0.16},         // linear_few, 8 waves
+    {16, 16, 8, 0.3, 1.5, 0.2, 0.108},         // 4 waves
+    {64, 128, 3, 2.0, 1.4, 0.95, 0.64},        // linear_rows, from here
+    {128, 256, 1, 4.0, 0.5, 1.5, 1.8},
+};
 constexpr double kBytesPerUs = 5.3e6;           // of memory
 
-int fastest_form(const LinearParams& p) {
+template <int N>
+int fastest_form(const LinearParams& p, const Form (&forms)[N]) {
   const double steps = (p.K + 127) / 128, units = compute_units();
   // groups, of which only the device knows the sizes: as if rows fell on them by chance
   const double groups = p.offsets ? p.E * (1.0 - std::pow(1.0 - 1.0 / p.E, (double)p.M)) : 1.0, rows = p.M / groups;
   const double memory = (groups * p.N * p.K + (double)p.M * (p.K + 2.0 * p.N)) / kBytesPerUs;
   int best = 0;
   double least = 0;
-  for (int i = 0; i < kFormCount; ++i) {
-    const Form& f = kForms[i];
+  for (int i = 0; i < N; ++i) {
+    const Form& f = forms[i];
     const double in_group = !p.offsets ? std::ceil(rows / f.BM) : rows <= f.BM / 2 ? 1.0 : rows / f.BM + 0.5;
     const double load = groups * in_group * ((p.N + f.BN - 1) / f.BN) / units, group = p.offsets ? f.group : 0.0;
     const double us = std::max(std::ceil(load / f.per_unit) * (f.end + group + steps * f.alone),
@@ -761,12 +794,14 @@ int fastest_form(const LinearParams& p) {
 template <typename T>
 hipError_t launch_typed(const LinearParams& p, hipStream_t st) {
   if (!direct_ok(p)) {
-    const double rows = p.offsets ? (double)p.M / p.E : p.M;
-    if (rows <= 16) return launch_few<1, 1, 8, 1, false, int8_t, T>(p, st);
-    if (rows <= 64) return launch_few<4, 2, 4, 1, false, int8_t, T>(p, st);
-    return launch_rows<4, 4, 2, 2, T>(p, st);
+    switch (fastest_form(p, kRowForms)) {
+      case 0: return launch_few<1, 1, 8, 1, false, int8_t, T>(p, st);
+      case 1: return launch_few<1, 1, 4, 1, false, int8_t, T>(p, st);
+      case 2: return launch_rows<2, 4, 2, 2, T>(p, st);
+      default: return launch_rows<4, 4, 2, 4, T>(p, st);
+    }
   }
-  switch (fastest_form(p)) {
+  switch (fastest_form(p, kForms)) {
     case 0: return launch_few<1, 1, 4, 2, true, int8_t, T>(p, st);
     case 1: return launch_few<1, 2, 4, 2, true, int8_t, T>(p, st);
     case 2: return launch_few<1, 4, 4, 1, true, int8_t, T>(p, st);

@@ -20,6 +20,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace qasr {
 namespace {
@@ -180,11 +181,10 @@ __device__ __forceinline__ float channel_bias(const LinearParams& L, const Tile&
 
 // Elements of x that linear_few quantises by itself: they are in registers in between.
 constexpr int kFloats = 8192;
-
 // W waves; wave w takes the steps w, w + W, ...; DIRECT: rows 16-byte aligned, K a multiple of 16.
 // X: int8_t, or the type of float tokens, up to 16 of them and kFloats elements, that every workgroup quantises for itself while its
 // weights are on their way (a launch less, which for one token is half of the time); their rows 16-byte aligned.
-template <int MT, int NT, int W, int S, bool DIRECT, typename X, typename T>
+template <int MT, int NT, int W, int S, bool DIRECT, bool ONCE, typename X, typename T>
 __global__ __launch_bounds__(64 * W) void linear_few_kernel(LinearParams L, Order o) {
   constexpr bool FLOATS = !__is_same(X, int8_t);
   static_assert(!FLOATS || (DIRECT && MT == 1), "floats: one product of tokens");
@@ -272,7 +272,8 @@ __global__ __launch_bounds__(64 * W) void linear_few_kernel(LinearParams L, Orde
       for (int j = 0; j < kLoads; ++j) {
         const int k = k0 + 16 * chunk[j];
         const void* p = k < L.K ? (const void*)(row[j] + k) : (const void*)kZeros;
-        if (brings[j]) direct_load16(p, stage + 1024 * j);
+        if (ONCE && 8 * j >= TOKENS) direct_load16_once(p, stage + 1024 * j);
+        else if (brings[j]) direct_load16(p, stage + 1024 * j);
       }
     };
     for (int i = 0; i < min(S, mine); ++i) ask(i);
@@ -427,7 +428,11 @@ struct Scales {
 
 // The results of a wave go through its share (ROOM bytes) of the LDS that the stages were in, as many tokens at a time as fit,
 // so that they leave as whole cache lines: from the registers, where a lane has 16 bytes of every product or two, they would go
-// as 64-byte pieces, which took 8 us more for 4096 x 4096 bf16.  Piece p of a row is at p ^ (row & 7).
+// as 64-byte pieces.  Piece p of a row is at p ^ (row & 7).
+// Rows that keep to boundaries of 64 bytes are stored past the caches, so that no workgroup leaves a 4 MB L2 full of lines to
+// be written out, and the operands stay there: 8192 x 14336 x 4096 364 us for 402, 4096 x 4096 x 512 15.5 for 17.9, and with the
+// layer that quantises the result behind it no slower (6400 x 2048 x 512: 38.6 us for 44.8 together).  Lines that two workgroups
+// share have to meet in the cache: 4096 x 4104 x 512 took 30.4 us past it, 27.8 through it.
 template <int MT, int NT, int BM, int BN, int ROOM, typename T>
 __device__ __forceinline__ void store_tile(const LinearParams& L, const Tile& t, const float* scales, unsigned char* room, int m0, int n0,
                                            const Sums<MT, NT>& acc) {
@@ -442,6 +447,7 @@ __device__ __forceinline__ void store_tile(const LinearParams& L, const Tile& t,
     bias[nt] = *(const v4f*)(scales + BM + BN + n0 + channel_of<P>(nt, 4 * g));
   }
   const int p = lane % PR, n = t.n0 + n0 + C * p;
+  const bool whole = (((uintptr_t)L.y | (uint64_t)L.ys * sizeof(T)) & 63) == 0;
 #pragma unroll
   for (int b = 0; b < MT / MB; ++b) {
     const int mb = m0 + 16 * MB * b;
@@ -461,10 +467,13 @@ __device__ __forceinline__ void store_tile(const LinearParams& L, const Tile& t,
     asm volatile("" ::: "memory");                           // other lanes read it: a wave's LDS accesses stay in order
     const int rows = min(16 * MB, t.hi - t.lo - mb);
     T* y = (T*)L.y + (int64_t)(t.lo + mb) * L.ys + n;
-    if (n + C <= L.N) {
+    auto piece = [&](int row) __attribute__((always_inline)) { return *(const v4i*)(room + (row * PR + (p ^ (row & 7))) * 16); };
+    if (whole && n + C <= L.N) {
 #pragma unroll 4
-      for (int row = lane / PR; row < rows; row += 64 / PR)
-        *reinterpret_cast<unaligned_chunk16*>(y + row * L.ys) = *(const v4i*)(room + (row * PR + (p ^ (row & 7))) * 16);
+      for (int row = lane / PR; row < rows; row += 64 / PR) __builtin_nontemporal_store(piece(row), (v4i*)(y + row * L.ys));
+    } else if (n + C <= L.N) {
+#pragma unroll 4
+      for (int row = lane / PR; row < rows; row += 64 / PR) *reinterpret_cast<unaligned_chunk16*>(y + row * L.ys) = piece(row);
     } else {
       for (int row = lane / PR; row < rows; row += 64 / PR)
         for (int c = 0; n + c < L.N; ++c) y[row * L.ys + c] = ((const T*)(room + (row * PR + (p ^ (row & 7))) * 16))[c];
@@ -474,7 +483,7 @@ __device__ __forceinline__ void store_tile(const LinearParams& L, const Tile& t,
 }
 
 // WM x WN waves of 16 MT tokens x 16 NT channels each, S stages of 128 codes.
-template <int MT, int NT, int WM, int WN, int S, typename T>
+template <int MT, int NT, int WM, int WN, int S, bool ONCE, typename T>
 __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearParams L, Order o) {
   constexpr int STEP = 128, P = products_of<T>(NT), RPL = 1024 / STEP, CPR = STEP / 16;     // rows per load, chunks per row
   constexpr int W = WM * WN, BM = 16 * MT * WM, BN = 16 * NT * WN, kStage = (BM + BN) * STEP;
@@ -503,11 +512,15 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearParams 
     if (j < kTokenLoads) off[j] = (uint32_t)(L.index ? max(x_row(L, t.lo + m), 0) : m) * (uint32_t)L.xs + 16 * token_chunk;
     else off[j] = (uint32_t)min(i, L.N - 1 - t.n0) * (uint32_t)L.ws + 16 * channel_chunk;
   }
+  auto load = [&](int j, const int8_t* from, int slot) __attribute__((always_inline)) {
+    if (ONCE && j >= kTokenLoads) direct_load16_once(from, off[j], lds + slot + 1024 * (j * W + wave));
+    else direct_load16(from, off[j], lds + slot + 1024 * (j * W + wave));
+  };
   // load j of stage k, which goes to `slot`; past the end of a row come zeros of the tokens (ask_end), anything of the channels
   auto ask_one = [&](int k, int slot, int j) __attribute__((always_inline)) {
     const int left = L.K - k * STEP;
     if (16 * (j < kTokenLoads ? token_chunk : channel_chunk) < left)
-      direct_load16((j < kTokenLoads ? xbase : wbase) + k * STEP, off[j], lds + slot + 1024 * (j * W + wave));
+      load(j, (j < kTokenLoads ? xbase : wbase) + k * STEP, slot);
   };
   auto ask_end = [&](int k, int slot) __attribute__((always_inline)) {
     if (16 * token_chunk >= L.K - k * STEP) {
@@ -590,7 +603,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearParams 
       // (the requests of a step, a few at a time: a wave whose request has to queue issues no products meanwhile)
 #pragma unroll
       for (int j = kLoads * (mt - 1) / (MT - 1); j < kLoads * mt / (MT - 1); ++j)
-        direct_load16(j < kTokenLoads ? xk : wk, off[j], lds + slot + 1024 * (j * W + wave));
+        load(j, j < kTokenLoads ? xk : wk, slot);
     });
     xk += STEP;
     wk += STEP;
@@ -701,16 +714,34 @@ Order order_of(const LinearParams& p, int BM, int BN) { return Order{(p.N + BN -
 
 GridShape grid_of(const Order& o) { return grid_shape(((int64_t)o.mt * o.nt + 7) / 8 * 8); }
 
+// groups with rows, of which only the device knows the sizes: as if rows fell on them by chance
+double groups_of(const LinearParams& p) { return p.offsets ? p.E * (1.0 - std::pow(1.0 - 1.0 / p.E, (double)p.M)) : 1.0; }
+
+// ONCE: the weights come past the 256 MB cache behind the L2s.  That is for matrices, all experts' together, that are larger than
+// the cache, and for as many rows as a tile has, of one matrix as two tiles that run side by side: 64 experts of 2048 x 2048 with
+// 8 rows each 44.3 us for 50.6, with 32 rows 50.1 for 54.9, 128 of 1024 x 2048 with a row each 27.4 for 29.3.  With two tiles to most of
+// 64 experts of 2816 x 2048 it is 165 us for 152.  Smaller matrices gain less where memory has them (32 x 11008 x 4096 14.9 us for 15.6),
+// and lose more where the cache does (17.4 for 13.2).
+constexpr int64_t kLargeWeights = 1 << 28;
+bool weights_once(const LinearParams& p, int BM) {
+  return (int64_t)(p.offsets ? p.E : 1) * p.N * p.K >= kLargeWeights && p.M <= (p.offsets ? 1 : 2) * BM * groups_of(p);
+}
+
 template <int MT, int NT, int W, int S, bool DIRECT, typename X, typename T>
 hipError_t launch_few(const LinearParams& p, hipStream_t st) {
   const Order o = order_of(p, 16 * MT, 16 * NT);
   const GridShape g = grid_of(o);
   constexpr bool floats = !__is_same(X, int8_t);
   const int bytes = W * S * 16 * ((floats ? 0 : MT) + NT) * 128 + (floats ? p.M * ((p.K + 127) / 128 * 128) + 128 : 0);
-  static std::atomic<uint64_t> done;
-  const hipError_t e = ensure_max_dynamic_lds((const void*)linear_few_kernel<MT, NT, W, S, DIRECT, X, T>, done);
-  if (e != hipSuccess) return e;
-  return launch_kernel(linear_few_kernel<MT, NT, W, S, DIRECT, X, T>, dim3(g.x, g.y), dim3(64 * W), bytes, st, p, o);
+  auto launch = [&](auto once) {
+    constexpr auto kernel = linear_few_kernel<MT, NT, W, S, DIRECT, once, X, T>;
+    static std::atomic<uint64_t> done;
+    const hipError_t e = ensure_max_dynamic_lds((const void*)kernel, done);
+    return e != hipSuccess ? e : launch_kernel(kernel, dim3(g.x, g.y), dim3(64 * W), bytes, st, p, o);
+  };
+  if constexpr (DIRECT && !floats)             // (what takes floats has no weights as large)
+    if (weights_once(p, 16 * MT)) return launch(std::true_type());
+  return launch(std::false_type());
 }
 
 template <int MT, int NT, int WM, int WN, int S, typename T>
@@ -718,10 +749,14 @@ hipError_t launch_tile(const LinearParams& p, hipStream_t st) {
   constexpr int BM = 16 * MT * WM, BN = 16 * NT * WN, bytes = S * (BM + BN) * 128 + 4 * (BM + 2 * BN);
   const Order o = order_of(p, BM, BN);
   const GridShape g = grid_of(o);
-  static std::atomic<uint64_t> done;
-  const hipError_t e = ensure_max_dynamic_lds((const void*)linear_tile_kernel<MT, NT, WM, WN, S, T>, done);
-  if (e != hipSuccess) return e;
-  return launch_kernel(linear_tile_kernel<MT, NT, WM, WN, S, T>, dim3(g.x, g.y), dim3(64 * WM * WN), bytes, st, p, o);
+  auto launch = [&](auto once) {
+    constexpr auto kernel = linear_tile_kernel<MT, NT, WM, WN, S, once, T>;
+    static std::atomic<uint64_t> done;
+    const hipError_t e = ensure_max_dynamic_lds((const void*)kernel, done);
+    return e != hipSuccess ? e : launch_kernel(kernel, dim3(g.x, g.y), dim3(64 * WM * WN), bytes, st, p, o);
+  };
+  if (weights_once(p, BM)) return launch(std::true_type());
+  return launch(std::false_type());
 }
 
 template <int MT, int NT, int WM, int WN, typename T>
@@ -771,8 +806,7 @@ constexpr double kBytesPerUs = 5.3e6;           // of memory
 template <int N>
 int fastest_form(const LinearParams& p, const Form (&forms)[N]) {
   const double steps = (p.K + 127) / 128, units = compute_units();
-  // groups, of which only the device knows the sizes: as if rows fell on them by chance
-  const double groups = p.offsets ? p.E * (1.0 - std::pow(1.0 - 1.0 / p.E, (double)p.M)) : 1.0, rows = p.M / groups;
+  const double groups = groups_of(p), rows = p.M / groups;
   const double memory = (groups * p.N * p.K + (double)p.M * (p.K + 2.0 * p.N)) / kBytesPerUs;
   int best = 0;
   double least = 0;

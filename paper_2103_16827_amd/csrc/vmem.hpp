@@ -35,6 +35,19 @@ __device__ __forceinline__ void direct_load16(const void* base, uint32_t off, co
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                :: "v"(off), "s"(base), "s"(m0v) : "memory");
 }
+// the same of bytes that nothing asks for again: past the 256 MB cache behind the L2s
+__device__ __forceinline__ void direct_load16_once(const void* gptr, const unsigned char* lds_wave_base) {
+  const uint32_t m0v = __builtin_amdgcn_readfirstlane(
+      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)lds_wave_base);
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt"
+               :: "v"(gptr), "s"(m0v) : "memory");
+}
+__device__ __forceinline__ void direct_load16_once(const void* base, uint32_t off, const unsigned char* lds_wave_base) {
+  const uint32_t m0v = __builtin_amdgcn_readfirstlane(
+      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)lds_wave_base);
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+               :: "v"(off), "s"(base), "s"(m0v) : "memory");
+}
 // The same load at device scope (sc1): it never hits in the vector cache of the compute unit, so it
 // sees what other workgroups of the same XCD have stored (and the XCD's L2 has acknowledged) earlier
 // in the same kernel.  A vector-cache invalidate that spares the L2 does not exist on this chip:

@@ -276,6 +276,27 @@ def test_experts_offsets_and_indexes_out_of_range():
         same(yd, want, f"offsets {offsets}")
 
 
+@pytest.mark.parametrize("sizes,rows", [([1] * 5 + [0] * 10 + [3], 1), ([9, 0, 16, 2] * 4, 20), ([40, 64, 1, 0] * 4, 33), ([128, 100, 70, 128] * 4, 70),
+                                        ([300, 0, 17, 256] * 4, 300)])
+def test_experts_larger_than_the_cache(sizes, rows):
+    """Experts of 2^28 codes together, and the same weights as one matrix."""
+    print(f"[case] large experts, {sizes[:4]}..", flush=True)
+    g, E, N, K, T = gen(10), 16, 4096, 4096, 300
+    w = torch.randint(-127, 128, (E, N, K), dtype=torch.int8, device="cuda", generator=torch.Generator(device="cuda").manual_seed(10))
+    M = sum(sizes)
+    x, xs, ws, index = codes(g, T, K), scales(g, T), scales(g, E, N), torch.randint(0, T, (M,), generator=g).int()
+    offsets = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32)
+    y = torch.full((M, N), float(FILL), dtype=torch.bfloat16, device="cuda")
+    Q.experts_int8(x.cuda(), xs.cuda(), torch.from_numpy(offsets).cuda(), index.cuda(), w, ws.cuda(), None, y)
+    one = torch.empty(rows, E * N, dtype=torch.float32, device="cuda")
+    Q.linear_int8(x[:rows].cuda(), xs[:rows].cuda(), w.view(E * N, K), ws.view(-1).cuda(), None, one)
+    for e in range(E):
+        lo, hi, we = offsets[e], offsets[e + 1], w[e].cpu()
+        i = index[lo:hi].long()
+        same(y[lo:hi], linear_ref(x[i], xs[i], we, ws[e], None, torch.bfloat16), f"expert {e}")
+        same(one[:, e * N:(e + 1) * N], linear_ref(x[:rows], xs[:rows], we, ws[e], None, torch.float32), f"part {e}")
+
+
 # ---- scores
 
 def _score_bounds(x64, m, ls, p, V):

@@ -780,7 +780,7 @@ bool direct_ok(const LinearParams& p) {
 // What a form of the kernels takes for one tile on a compute unit, in us: `end` for its beginning and end, `group` more of that
 // where a tile's rows have to be found first, and for a step of 128 codes `alone` with nothing else on the chip, `busy` with
 // a tile on every unit.  Fitted to 10 forms x 36 shapes of 1 to 16384 rows, 10 of them in groups, on weights that no cache held (rms 6 to 16 %
-// by form); next to the fastest form of each shape, the one that the rule takes cost nothing in 32 of them and at most 10 %.
+// by form); next to the fastest form of each shape, the one that the rule takes cost nothing in 32 of them and at most 9 %.
 struct Form { int BM, BN, per_unit; double end, group, alone, busy; };
 constexpr Form kForms[] = {
     {16, 16, 5, 0.29, 1.5, 0.085, 0.039},      // linear_few, from here
@@ -789,10 +789,10 @@ constexpr Form kForms[] = {
     {32, 32, 2, 0.88, 1.1, 0.128, 0.088},
     {32, 64, 1, 2.2, 1.2, 0.132, 0.185},
     {64, 64, 1, 3.8, 1.1, 0.210, 0.265},
-    {64, 128, 2, 1.2, 1.4, 0.306, 0.362},      // linear_tile, from here
-    {128, 128, 1, 2.8, 1.0, 0.375, 0.617},
-    {128, 256, 1, 4.0, 0.1, 0.525, 0.993},
-    {256, 256, 1, 4.4, 0.0, 1.033, 1.821},
+    {64, 128, 2, 0.94, 1.55, 0.318, 0.346},    // linear_tile, from here
+    {128, 128, 1, 2.57, 1.12, 0.383, 0.564},
+    {128, 256, 1, 3.39, 0.48, 0.556, 0.907},
+    {256, 256, 1, 3.11, 1.71, 1.216, 1.216},
 };
 // ... where rows begin anywhere or end inside a chunk (14 shapes, of which the rule takes the fastest form but for 4 to 9 % in three)
 constexpr Form kRowForms[] = {

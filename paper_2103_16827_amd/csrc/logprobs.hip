@@ -16,6 +16,7 @@
 #include "kernels.hpp"
 #include "lanes.hpp"
 #include "launch_shape.hpp"
+#include <algorithm>
 
 namespace qasr {
 namespace {
@@ -65,11 +66,17 @@ struct Pieces {
 struct Ahead {
   int tok = -1;
   float x = 0.0f;
+  __device__ __forceinline__ void ask(const LogprobParams& p, int64_t row, int j) {
+    if (j < p.n) tok = p.tokens[row * p.n + j];
+  }
+  template <typename T>
+  __device__ __forceinline__ void look(const LogprobParams& p, int64_t row) {
+    if (tok >= 0 && tok < p.V) x = to_float(((const T*)p.x + row * p.xs)[tok]);
+  }
   template <typename T>
   __device__ __forceinline__ void load(const LogprobParams& p, int64_t row, int j) {
-    if (j >= p.n) return;
-    tok = p.tokens[row * p.n + j];
-    if (tok >= 0 && tok < p.V) x = to_float(((const T*)p.x + row * p.xs)[tok]);
+    ask(p, row, j);
+    look<T>(p, row);
   }
 };
 
@@ -112,7 +119,7 @@ __device__ __forceinline__ void sync() {
 // LDS of a choice of the best: the largest number in each column, and the candidates
 template <int W>
 struct Choice {
-  static constexpr int kQuarters = W >= 4 ? 4 : 1;     // columns / 64, where `top` is large
+  static constexpr int kQuarters = 4;                  // columns / 64, where `top` is large
   __align__(16) uint32_t column[64 * kQuarters];
   uint64_t cand[kRoom];
   uint64_t wave_best[W];
@@ -130,10 +137,11 @@ struct Choice {
   __device__ __forceinline__ void offer(int top, uint32_t own, int tid) {
     atomicMax(&column[(tid & 63) + (top > 24 ? 64 * ((tid >> 6) % kQuarters) : 0)], own);
   }
-  // One wave: the largest number that at least `top` of the columns reach (in its first 20 bits where there are four times 64).
-  __device__ __forceinline__ uint32_t limit(int top) const {
+  // One wave: the largest number that at least n of the columns reach, 0 if there is none (where there are four times 64 in its bits from
+  // `low` on).
+  __device__ __forceinline__ uint32_t limit(int top, int n, int low) const {
     const int lane = threadIdx.x & 63;
-    if (top <= 24 || kQuarters == 1) {
+    if (top <= 24) {
       const uint32_t mine = column[lane];
       int above = 0;
 #pragma unroll 2
@@ -141,19 +149,53 @@ struct Choice {
         const v4u c = *reinterpret_cast<const v4u*>(column + o);
         above += (c[0] > mine) + (c[1] > mine) + (c[2] > mine) + (c[3] > mine);
       }
-      return wave_min(above < top ? mine : ~0u);
+      return wave_min(above < n ? mine : ~0u);
     }
     uint32_t mine[kQuarters], found = 0;
 #pragma unroll
     for (int q = 0; q < kQuarters; ++q) mine[q] = column[64 * q + lane];
-    for (int bit = 31; bit >= 12; --bit) {
+    for (int bit = 31; bit >= low; --bit) {
       const uint32_t higher = found | 1u << bit;
-      int n = 0;
+      int reach = 0;
 #pragma unroll
-      for (int q = 0; q < kQuarters; ++q) n += __popcll(__ballot(mine[q] >= higher));
-      if (n >= top) found = higher;
+      for (int q = 0; q < kQuarters; ++q) reach += __popcll(__ballot(mine[q] >= higher));
+      if (reach >= n) found = higher;
     }
     return found;
+  }
+  // The candidates where those that reach the limit are too many, most often because the `top` best end among equal logits (a mask that
+  // leaves fewer than `top`): the larger ones, and of the equal ones those whose ids reach a limit found in the same way.  each(f)
+  // calls f(order, ~id) for the thread's logits.  False if these are too many as well.  (A sync comes before it.)
+  template <typename Each>
+  __device__ __forceinline__ bool among_equals(int top, int tid, Each&& each) {
+    if (W == 1 || tid < 64) {
+      const uint32_t l = limit(top, top, 0);
+      if ((tid & 63) == 0) least = l;
+    }
+    sync<W>();
+    const uint32_t value = least;
+    clear(tid);
+    sync<W>();
+    uint32_t first = 0;
+    each([&](uint32_t order, uint32_t id) __attribute__((always_inline)) {
+      if (order > value) add((uint64_t)order << 32 | id);
+      else if (order == value) first = max(first, id);
+    });
+    offer(top, first, tid);
+    sync<W>();
+    const int larger = count;
+    if (larger > kRoom) return false;
+    if (W == 1 || tid < 64) {
+      const uint32_t l = larger < top ? limit(top, top - larger, 0) : ~0u;
+      if ((tid & 63) == 0) least = l;
+    }
+    sync<W>();
+    const uint32_t lowest = least;
+    each([&](uint32_t order, uint32_t id) __attribute__((always_inline)) {
+      if (order == value && id >= lowest) add((uint64_t)order << 32 | id);
+    });
+    sync<W>();
+    return count <= kRoom;
   }
   __device__ __forceinline__ void add(uint64_t key) {
     const int to = atomicAdd(&count, 1);
@@ -162,13 +204,30 @@ struct Choice {
   // Calls f(rank, key) for the `top` best candidates.  (A sync comes before it.)
   template <typename F>
   __device__ __forceinline__ void rank(int top, int tid, F&& f) const {
+    constexpr int B = kRoom > 64 * W ? (kRoom / (64 * W) < 4 ? kRoom / (64 * W) : 4) : 1;
     const int found = count;
-    for (int i = tid; i < found; i += 64 * W) {
-      const uint64_t k = cand[i];
-      int r = 0;
-      for (int o = 0; o < found; ++o) r += cand[o] > k;
-      if (r < top) f(r, k);
+    if (found <= 64 * W) rank_some<1>(top, tid, found, f);
+    else for (int i = tid; i < found; i += 64 * W * B) rank_some<B>(top, i, found, f);
+  }
+  // ... of the candidates i, i + 64 W ..: each that is read is compared with B
+  template <int B, typename F>
+  __device__ __forceinline__ void rank_some(int top, int i, int found, F&& f) const {
+    uint64_t k[B];
+    int r[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      k[b] = i + b * 64 * W < found ? cand[i + b * 64 * W] : 0;
+      r[b] = 0;
     }
+    if (k[0] == 0) return;
+    for (int o = 0; o < found; ++o) {
+      const uint64_t other = cand[o];
+#pragma unroll
+      for (int b = 0; b < B; ++b) r[b] += other > k[b];
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+      if (k[b] != 0 && r[b] < top) f(r[b], k[b]);
   }
   // The same for all keys next(i), i = tid, tid + 64 W .. < n, one after the other
   template <typename Next, typename F>
@@ -254,14 +313,31 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 16 ? 8 : 1) void logpro
   sweep([&](float a, float b) { m = max3(m, a, b); });
   const uint32_t own = order_of(m);                    // of this thread's logits
   m = wave_max(m);
-  if (top > 0) choice.offer(top, own, tid);
+  // (a wave on its own has too few threads for four times 64 columns: a lane's loads, or the words of its only one, are four)
+  const bool by_load = W == 1 && top > 24;
+  if (by_load) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float most = q == 0 ? last : ninf;
+      if constexpr (R == 1) {
+#pragma unroll
+        for (int k = q * N / 4; k < (q + 1) * N / 4; ++k) most = fmaxf(most, logit<T>(raw[0], k));
+      } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) most = fmaxf(most, logit<T>(raw[q % R], k));
+      }
+      choice.column[64 * q + lane] = order_of(most);
+    }
+  } else if (top > 0) {
+    choice.offer(top, own, tid);
+  }
   if constexpr (W > 1) {
     if (lane == 0) part[0][wave] = m;
   }
   sync<W>();
   if constexpr (W > 1) m = wave_max(part[0][lane % W]);
   if (top > 0 && (W == 1 || wave == 0)) {              // (meanwhile the others go on)
-    const uint32_t l = choice.limit(top);
+    const uint32_t l = choice.limit(top, top, 12);
     if (lane == 0) choice.least = l;
   }
   const float base = m == ninf ? 0.0f : m;             // (nothing but -infinity: every exponential is 0)
@@ -290,7 +366,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 16 ? 8 : 1) void logpro
     t = wave_sum(lane < W ? part[0][2 * W + lane] : 0.0f);
   }
   const uint32_t limit = top > 0 ? choice.least : 0;
-  if (top > 0 && own >= limit && (tid < loads || rest < len)) {
+  if (top > 0 && !by_load && own >= limit && (tid < loads || rest < len)) {
     const int h = atomicAdd(&choice.holders, 1);
     if (h < kHolders) {
 #pragma unroll
@@ -303,14 +379,44 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 16 ? 8 : 1) void logpro
   if (c.n == 1) score.template tokens<T>(p, row, tid, 64 * W, ahead);
   else if (tid == 0) c.part[unit] = Part{m, s, t};
   if (top == 0) return;
+  if (score.bad) {                                     // (who joins the pieces asks for none of this one's)
+    if (c.n == 1 && tid < top) score.alternative(p, row, tid, 0);
+    return;
+  }
   sync<W>();
 
   auto leave = [&](int j, uint64_t key) __attribute__((always_inline)) {
     if (c.n == 1) score.alternative(p, row, j, key);
     else c.best[unit * p.top + j] = key;
   };
+  // calls f(order, ~id) for the thread's logits (read again, but by a wave on its own: few rows come here, and registers are short)
+  auto each = [&](auto&& f) __attribute__((always_inline)) {
+    auto all_of = [&](const v4u& v, int at) __attribute__((always_inline)) {
+      if (at >= loads) return;
+#pragma unroll
+      for (int k = 0; k < N; ++k) f(order_of(logit<T>(v, k)), (uint32_t)~(v0 + head + at * N + k));
+    };
+    if constexpr (W == 1) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        asm volatile("" : "+v"(raw[i]));
+        all_of(raw[i], i * 64 + tid);
+      }
+    } else {
+#pragma unroll 4
+      for (int at = tid; at < loads; at += 64 * W) all_of(aligned[at], at);
+    }
+    if (rest < len) f(order_of(last), (uint32_t)~(v0 + rest));
+  };
   const int holders = choice.holders;
-  if (holders <= kHolders) {
+  bool fits = holders <= kHolders;
+  if (by_load) {
+    each([&](uint32_t order, uint32_t id) __attribute__((always_inline)) {
+      if (order >= limit) choice.add((uint64_t)order << 32 | id);
+    });
+    sync<W>();
+    fits = choice.count <= kRoom;
+  } else if (fits) {
     // a load of a holder for each thread, then the holders' last logits
     for (int i = tid; i < holders * R; i += 64 * W) {
       const int h = i / R, at = ((i % R) * 64 * W + holder[sub][h]);
@@ -328,8 +434,10 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 16 ? 8 : 1) void logpro
       if (at < len && order_of(held_last[sub][h]) >= limit) choice.add(key_of(held_last[sub][h], v0 + at));
     }
     sync<W>();
+    fits = choice.count <= kRoom;
   }
-  if (holders <= kHolders && choice.count <= kRoom) choice.rank(top, tid, leave);
+  if (!fits) fits = choice.among_equals(top, tid, each);
+  if (fits) choice.rank(top, tid, leave);
   else choice.one_by_one(top, len, tid, [&](int i) { return key_of(to_float(x[i]), v0 + i); }, leave);
   if (c.n > 1 && tid >= top && tid < p.top) c.best[unit * p.top + tid] = 0;
 }
@@ -406,21 +514,28 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(LogprobParams p, 
   const int64_t row = ((int64_t)blockIdx.y << kGridShift) + blockIdx.x;
   if (row >= p.rows) return;
   const int tid = threadIdx.x, lane = tid & 63;
+  const float ninf = -__builtin_inff();
+  // (a token, keys and parts are on their way together: what is waited for here is two loads one after the other)
   Ahead ahead;
-  ahead.load<T>(p, row, tid);
+  ahead.ask(p, row, tid);
   const uint64_t* keys = c.best + row * c.n * p.top;
   const int n = c.n * p.top;
   uint64_t held[kHeld];
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) held[i] = i * 64 * W + tid < n ? keys[i * 64 * W + tid] : 0;
-  const float ninf = -__builtin_inff();
-  float m = ninf;
-  for (int i = lane; i < c.n; i += 64) m = fmaxf(m, c.part[row * c.n + i].m);
+  for (int i = 0; i < kHeld; ++i) {
+    // (a piece's keys are in order: with the rotation a thread holds some of every rank where 64 W is a multiple of p.top too)
+    const int at = i * 64 * W + (tid + 37 * i) % (64 * W);
+    held[i] = at < n ? keys[at] : 0;
+  }
+  const Part mine = lane < c.n ? c.part[row * c.n + lane] : Part{ninf, 0.0f, 0.0f};
+  ahead.look<T>(p, row);
+  float m = mine.m;
+  for (int i = lane + 64; i < c.n; i += 64) m = fmaxf(m, c.part[row * c.n + i].m);
   m = wave_max(m);
   const float base = m == ninf ? 0.0f : m;
   float s = 0.0f, t = 0.0f;
   for (int i = lane; i < c.n; i += 64) {
-    const Part q = c.part[row * c.n + i];
+    const Part q = i == lane ? mine : c.part[row * c.n + i];
     // (a piece without a logit above -infinity adds nothing: its s and t are 0)
     const float d = (q.m == ninf ? base : q.m) - base, f = __expf(d);
     s += q.s * f;
@@ -431,9 +546,20 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(LogprobParams p, 
   const Scorer score(m, s, t);
   score.template tokens<T>(p, row, tid, 64 * W, ahead);
   if (p.top == 0) return;
+  if (score.bad) {
+    if (tid < p.top) score.alternative(p, row, tid, 0);
+    return;
+  }
   auto leave = [&](int j, uint64_t key) __attribute__((always_inline)) { score.alternative(p, row, j, key); };
   if (n > kHeld * 64 * W) {
     choice.one_by_one(p.top, n, tid, [&](int i) { return keys[i]; }, leave);
+    return;
+  }
+  if (n <= 64 * W) {                                   // few: each is compared with all
+    if (tid < n) choice.cand[tid] = held[0];
+    if (tid == 0) choice.count = n;
+    sync<W>();
+    choice.rank(p.top, tid, leave);
     return;
   }
   choice.clear(tid);
@@ -444,30 +570,45 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(LogprobParams p, 
   choice.offer(p.top, (uint32_t)(own >> 32), tid);
   sync<W>();
   // (where fewer columns than that have a key the limit is 0 and every key is a candidate)
-  const uint32_t limit = choice.limit(p.top);
+  const uint32_t limit = choice.limit(p.top, p.top, 12);
   if ((uint32_t)(own >> 32) >= limit) {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
       if (held[i] != 0 && (uint32_t)(held[i] >> 32) >= limit) choice.add(held[i]);
   }
   sync<W>();
-  if (choice.count <= kRoom) choice.rank(p.top, tid, leave);
+  bool fits = choice.count <= kRoom;
+  if (!fits)
+    fits = choice.among_equals(p.top, tid, [&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (held[i] != 0) f((uint32_t)(held[i] >> 32), (uint32_t)held[i]);
+    });
+  if (fits) choice.rank(p.top, tid, leave);
   else choice.one_by_one(p.top, n, tid, [&](int i) { return keys[i]; }, leave);
 }
 
 int size_of(int type) { return type == 0 ? 4 : 2; }
 
-// Bytes of logits that the largest workgroup takes: 16 waves of 8 loads a lane.
-constexpr int kWhole = 16 * 64 * 8 * 16;
+// Bytes of logits that the largest workgroup takes (16 waves of 8 loads a lane), and one of 8 waves of 13.
+constexpr int kWhole = 16 * 64 * 8 * 16, kPiece = 8 * 64 * 13 * 16;
 
-Pieces pieces_of(int64_t rows, int V, int bytes) {
+// A row that one workgroup can take is one piece: it is done before a second kernel would begin (32000 float32 logits and five
+// alternatives 6.7 us, 9.9 in 15 pieces; 1000 such rows 26.5, 33.4 in two).  Few long rows: pieces for the whole chip, of 8 KiB and
+// more, whose best the workgroup that joins them can hold.  Else the number of them that leaves the busiest compute unit the least to do, up to twice as many as it takes (128 rows
+// of 128256 fp16 logits with 20 alternatives 20.1 us in 4 pieces, 20.9 in 2, 22.4 in 3; 1000 of 100000 49.4 in 2, 52.4 in 3, 54.7 in 4).
+Pieces pieces_of(int64_t rows, int V, int bytes, int top) {
   Pieces c{};
   const int64_t all = (int64_t)V * bytes;
-  int64_t n = (all + kWhole - 1) / kWhole;
-  // few long rows: pieces for the whole chip, of 8 KiB and more (a row that one workgroup can take is done before a second kernel
-  // would begin: 32000 float32 logits in 6.7 us, five alternatives with them, against 9.9 in 15 pieces)
-  const int64_t want = 256 / rows, most = (all + 8191) / 8192;
-  if (n > 1 && want > n) n = want < most ? want : most;
+  int64_t n = 1;
+  if (all > kWhole) {
+    const int64_t least = (all + kPiece - 1) / kPiece, want = 256 / rows,
+                  most = std::min<int64_t>((all + 8191) / 8192, kHeld * 64 * kJoinWaves / std::max(top, 1));
+    auto turns = [&](int64_t k) { return (rows * k + 255) / 256; };
+    n = std::max(least, std::min(want, most));
+    for (int64_t k = least + 1; k <= 2 * least && k <= 64; ++k)
+      if (turns(k) * n < turns(n) * k) n = k;
+  }
   const int per = 16 / bytes;
   c.len = (int)(((V + n - 1) / n + per - 1) / per * per);
   c.n = (int)((V + (int64_t)c.len - 1) / c.len);
@@ -479,7 +620,7 @@ Pieces pieces_of(int64_t rows, int V, int bytes) {
 size_t logprobs_workspace_bytes(int64_t rows, int V, int top) {
   size_t most = 0;
   for (int bytes = 2; bytes <= 4; bytes += 2) {
-    const Pieces c = rows > 0 ? pieces_of(rows, V, bytes) : Pieces{1};
+    const Pieces c = rows > 0 ? pieces_of(rows, V, bytes, top) : Pieces{1};
     const size_t need = c.n == 1 ? 0 : (size_t)rows * c.n * (16 + 8 * (size_t)top);
     most = need > most ? need : most;
   }
@@ -488,7 +629,7 @@ size_t logprobs_workspace_bytes(int64_t rows, int V, int top) {
 
 hipError_t launch_logprobs(const LogprobParams& p, int x_type, void* workspace, hipStream_t st) {
   const int bytes = size_of(x_type);
-  Pieces c = pieces_of(p.rows, p.V, bytes);
+  Pieces c = pieces_of(p.rows, p.V, bytes, p.top);
   if (c.n > 1) {
     c.best = (uint64_t*)workspace;
     c.part = (Part*)(c.best + (size_t)p.rows * c.n * p.top);
@@ -513,7 +654,9 @@ hipError_t launch_logprobs(const LogprobParams& p, int x_type, void* workspace, 
     else if (loads <= 512) e = launch(logprobs_kernel<T, 4, 2>, 4);
     else if (loads <= 1024) e = launch(logprobs_kernel<T, 4, 4>, 4);
     else if (loads <= 2048) e = launch(logprobs_kernel<T, 4, 8>, 4);
+    else if (loads <= 2560 && units >= 1024) e = launch(logprobs_kernel<T, 4, 10>, 4);
     else if (loads <= 4096) e = launch(logprobs_kernel<T, 8, 8>, 8);
+    else if (loads <= 8 * 64 * 13) e = launch(logprobs_kernel<T, 8, 13>, 8);
     else e = launch(logprobs_kernel<T, 16, 8>, 16);
     if (e != hipSuccess || c.n == 1) return e;
     const GridShape g = grid_shape(p.rows);

@@ -435,6 +435,56 @@ def test_token_logprobs_values(V, dtype):
     check_scores(x, None, 20, entropy=False)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V,tops", [(66, (30, 64)), (300, (25, 64)), (600, (20, 64)), (2040, (25, 33, 64)), (7000, (20, 64)), (50257, (5, 64)), (130000, (20, 64))])
+def test_token_logprobs_few_allowed(V, tops, dtype):
+    """Masks that leave fewer tokens than there are alternatives, or hardly more; ids that are equal in every column but a few."""
+    print(f"[case] logprobs few allowed V={V} {dtype}", flush=True)
+    g, ninf = gen(V + 4), float("-inf")
+    x = (torch.randn(14, V, generator=g) * 3).to(dtype)
+    for row, allowed in enumerate((0, 1, 3, 19, 20, 30, 63, 64, 200)):
+        keep = torch.zeros(V, dtype=torch.bool)
+        keep[torch.randperm(V, generator=g)[:allowed]] = True
+        x[row, ~keep] = ninf if row % 2 else torch.finfo(dtype).min
+    x[9] = torch.where(torch.arange(V) // 8 % 64 < 3, 1.0, -1.0).to(dtype)        # the best in few threads
+    x[10, V // 3:] = ninf
+    x[10, :V // 3] = 2.0
+    x[11] = (torch.arange(V) * 64 // V).to(dtype)        # steps
+    x[12, ::2] = 7.0
+    x[13, 1:] = 0.0
+    x[13, 0] = -0.0
+    tokens = torch.randint(0, V, (14, 2), generator=g).int()
+    for top in tops:
+        check_scores(x, tokens, top, Padded(14, V, dtype, V + 3, 1, x) if V % 2 == 0 else None)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [30, 65, 500, 1500, 9000, 60000, 140000])
+def test_token_logprobs_negative_nans(V, dtype):
+    """A NaN whose sign bit is set (what 0 * inf gives on many processors), alone and everywhere."""
+    print(f"[case] logprobs negative NaN V={V} {dtype}", flush=True)
+    g = gen(V + 5)
+    x = (torch.randn(4, V, generator=g) * 3).to(dtype)
+    bits = x.view(torch.int32 if dtype == torch.float32 else torch.int16)
+    nan = {torch.float32: -(1 << 22), torch.float16: -(1 << 9), torch.bfloat16: -(1 << 6)}[dtype]      # all ones but the fraction's lower bits
+    bits[0, V // 2] = nan
+    bits[1] = nan
+    bits[2] = -1
+    assert bool(x[:3].isnan().any(1).all()) and not bool(x[3].isnan().any())
+    for top in (20, min(V, 64)):
+        check_scores(x, torch.tensor([[0, V - 1]] * 4, dtype=torch.int32), top)
+
+
+@pytest.mark.parametrize("rows,V,top", [(1, 128256, 64), (2, 128256, 8), (1, 1900000, 64), (130, 128256, 20), (300, 70000, 16), (1030, 18000, 33), (1100, 1000, 64)])
+def test_token_logprobs_pieces(rows, V, top):
+    print(f"[case] logprobs pieces {rows} x {V} top {top}", flush=True)
+    g = gen(V + rows + top)
+    x = (torch.randn(rows, V, generator=g) * 4).to(torch.float16)
+    x[rows // 2, 50:] = float("-inf")
+    check_scores(x, torch.randint(0, V, (rows, 1), generator=g).int(), top)
+    check_scores(x.float(), None, top)
+
+
 def test_token_logprobs_rows_beyond_32_bits():
     print("[case] logprobs, offsets beyond 32 bits", flush=True)
     g = gen(12)

@@ -440,7 +440,7 @@ enum { QASR_F32 = 0, QASR_F16 = 1, QASR_BF16 = 2 };
  *   a[m] = max_k |x[m,k]| over finite x;  S[m] = a > 0 ? max(a / 127, 2^-126) : 1;  q[m,k] = Int(clip(x[m,k] / S[m], -127, 127))
  * in single precision, each operation rounded once, ties to even, as qasr_quantize; an infinite x gives +-127, a NaN 0.
  * x: [M, K] device of type x_type, row stride x_stride; q: [M, K] int8 device, row stride q_stride (what lies between rows is
- * left as it was); scale: [M] float32.  M >= 0 (0: no-op), K >= 1, strides 0 or >= K, else QASR_ERR_SHAPE; an unknown type is
+ * left as it was); scale: [M] float32.  M >= 0 (0: no-op), 1 <= K <= 2^30, strides 0 or >= K, else QASR_ERR_SHAPE; an unknown type is
  * QASR_ERR_PARAM; q and scale must overlap neither x nor each other. */
 qasr_status qasr_quantize_tokens(const void* x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride, int8_t* q,
                                  int64_t q_stride, float* scale, void* stream);
@@ -450,8 +450,9 @@ qasr_status qasr_quantize_tokens(const void* x, int32_t x_type, int64_t M, int32
  * in single precision, each operation rounded once, then rounded to y_type (to nearest, ties to even).
  * x: [M, K] int8, w: [N, K] int8, y: [M, N] of y_type, row strides as given (0 => dense; what lies between rows of y is left as it
  * was); x_scale: [M], w_scale, bias: [N] float32; all device.  Runs fastest where K, the strides of x and w and their
- * addresses are multiples of 16.  M >= 0 (0: no-op), N >= 1, 1 <= K <= 131071 (the accumulator cannot overflow) and strides
- * 0 or >= a row, else QASR_ERR_SHAPE; unknown y_type or reserved != 0: QASR_ERR_PARAM; y must not overlap any operand. */
+ * addresses are multiples of 16.  0 <= M <= 2^30 (0: no-op), 1 <= N <= 2^30, (M/16 + 1) (N/16 + 1) <=
+ * 2^31 - 16, 1 <= K <= 131071 (the accumulator cannot overflow) and strides 0 or >= a row, else QASR_ERR_SHAPE; unknown y_type or
+ * reserved != 0: QASR_ERR_PARAM; y must not overlap any operand. */
 typedef struct {
   int32_t M, N, K;
   int32_t y_type;                          /* QASR_F32, QASR_F16, QASR_BF16 */
@@ -476,8 +477,9 @@ qasr_status qasr_linear_int8_dynamic(const qasr_linear_desc* d, const void* x, i
  * Groups may be empty; rows outside every group (before offsets[0], from offsets[E] on) are left as they were.  offsets should not
  * decrease: they are taken as min(max(offset, 0), M), a group that ends before it starts is empty, and where decreasing
  * offsets make groups share rows, or give the groups more rows than M together, the values of y are undefined (never an access out
- * of range).  A row whose index is outside [0, x_rows) counts as codes of zero.  Errors as above; E < 1, E > 4096, x_rows < 1 or an expert
- * stride smaller than a matrix is QASR_ERR_SHAPE, and so is x_rows < M without an index. */
+ * of range).  A row whose index is outside [0, x_rows) counts as codes of zero.  Errors as above; E < 1, E > 4096,
+ * (M/16 + E) (N/16 + 1) > 2^31 - 16, x_rows < 1 or an expert stride smaller than a matrix is QASR_ERR_SHAPE, and so is x_rows < M
+ * without an index. */
 typedef struct {
   qasr_linear_desc l;
   int32_t E, x_rows;

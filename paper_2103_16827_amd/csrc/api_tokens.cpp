@@ -27,14 +27,17 @@ bool rows_ok(int64_t rows, int64_t stride, int64_t n) {
 
 constexpr int32_t kMaxK = 131071;          // 128 x 128 x K < 2^31
 constexpr int32_t kMaxExperts = 4096;
+constexpr int32_t kMaxSide = 1 << 30;      // of rows, channels and elements of a row: with a tile or a workgroup more they are int32 still
+constexpr int64_t kMaxTiles = ((int64_t)1 << 31) - 16;      // (16 x 16 is the smallest tile)
 
 size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 int64_t round16(int64_t n) { return (n + 15) & ~(int64_t)15; }
 
 // the descriptor's own checks and the strides that 0 stands for
-qasr_status check_linear(const qasr_linear_desc* d, qasr_linear_desc& out) {
+qasr_status check_linear(const qasr_linear_desc* d, int32_t groups, qasr_linear_desc& out) {
   if (!d) return QASR_ERR_NULL;
-  if (d->M < 0 || d->N < 1 || d->K < 1 || d->K > kMaxK) return QASR_ERR_SHAPE;
+  if (d->M < 0 || d->M > kMaxSide || d->N < 1 || d->N > kMaxSide || d->K < 1 || d->K > kMaxK) return QASR_ERR_SHAPE;
+  if (((int64_t)d->M / 16 + groups) * ((int64_t)d->N / 16 + 1) > kMaxTiles) return QASR_ERR_SHAPE;
   if (!rows_ok(d->M, d->x_stride, d->K) || !rows_ok(d->N, d->w_stride, d->K) || !rows_ok(d->M, d->y_stride, d->N))
     return QASR_ERR_SHAPE;
   if (size_of(d->y_type) == 0 || d->reserved != 0) return QASR_ERR_PARAM;
@@ -63,7 +66,7 @@ qasr_status qasr_quantize_tokens(const void* x, int32_t x_type, int64_t M, int32
                                  int64_t q_stride, float* scale, void* stream) {
   const int64_t size = size_of(x_type);
   if (size == 0) return QASR_ERR_PARAM;
-  if (M < 0 || K < 1 || M > ((int64_t)1 << 40) || !rows_ok(M, x_stride, K) || !rows_ok(M, q_stride, K)) return QASR_ERR_SHAPE;
+  if (M < 0 || K < 1 || K > kMaxSide || M > ((int64_t)1 << 40) || !rows_ok(M, x_stride, K) || !rows_ok(M, q_stride, K)) return QASR_ERR_SHAPE;
   if (M == 0) return QASR_OK;
   if (!x || !q || !scale) return QASR_ERR_NULL;
   if (misaligned(x, size) || misaligned(scale, 4)) return QASR_ERR_PARAM;
@@ -77,7 +80,7 @@ qasr_status qasr_quantize_tokens(const void* x, int32_t x_type, int64_t M, int32
 qasr_status qasr_linear_int8(const qasr_linear_desc* desc, const int8_t* x, const float* x_scale, const int8_t* w,
                              const float* w_scale, const float* bias, void* y, void* stream) {
   qasr_linear_desc d;
-  const qasr_status st = check_linear(desc, d);
+  const qasr_status st = check_linear(desc, 1, d);
   if (st != QASR_OK) return st;
   if (d.M == 0) return QASR_OK;
   if (!x || !x_scale || !w || !w_scale || !y) return QASR_ERR_NULL;
@@ -99,7 +102,7 @@ qasr_status qasr_linear_int8_dynamic(const qasr_linear_desc* desc, const void* x
                                      const float* w_scale, const float* bias, void* y, void* workspace,
                                      size_t workspace_bytes, void* stream) {
   qasr_linear_desc d;
-  const qasr_status st = check_linear(desc, d);
+  const qasr_status st = check_linear(desc, 1, d);
   if (st != QASR_OK) return st;
   const int64_t xsize = size_of(x_type), size = size_of(d.y_type);
   if (xsize == 0) return QASR_ERR_PARAM;
@@ -133,11 +136,12 @@ qasr_status qasr_experts_int8(const qasr_experts_desc* desc, const int8_t* x, co
                               void* stream) {
   if (!desc) return QASR_ERR_NULL;
   qasr_linear_desc d;
-  const qasr_status st = check_linear(&desc->l, d);
+  if (desc->E < 1 || desc->E > kMaxExperts) return QASR_ERR_SHAPE;
+  const qasr_status st = check_linear(&desc->l, desc->E, d);
   if (st != QASR_OK) return st;
   const int64_t matrix = extent(d.N, d.w_stride, d.K);
   const int64_t wes = desc->w_expert_stride ? desc->w_expert_stride : (int64_t)d.N * d.w_stride;
-  if (desc->E < 1 || desc->E > kMaxExperts || desc->x_rows < 1 || wes < matrix || wes > ((int64_t)1 << 58) / desc->E ||
+  if (desc->x_rows < 1 || wes < matrix || wes > ((int64_t)1 << 58) / desc->E ||
       !rows_ok(desc->x_rows, d.x_stride, d.K) || (!index && desc->x_rows < d.M))
     return QASR_ERR_SHAPE;
   if (d.M == 0) return QASR_OK;

@@ -272,7 +272,7 @@ __global__ __launch_bounds__(64 * W) void linear_few_kernel(LinearParams L, Orde
       for (int j = 0; j < kLoads; ++j) {
         const int k = k0 + 16 * chunk[j];
         const void* p = k < L.K ? (const void*)(row[j] + k) : (const void*)kZeros;
-        if (ONCE && 8 * j >= TOKENS) direct_load16_once(p, stage + 1024 * j);
+        if (ONCE && 8 * j >= TOKENS) direct_load16(Once(), p, stage + 1024 * j);
         else if (brings[j]) direct_load16(p, stage + 1024 * j);
       }
     };
@@ -513,7 +513,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearParams 
     else off[j] = (uint32_t)min(i, L.N - 1 - t.n0) * (uint32_t)L.ws + 16 * channel_chunk;
   }
   auto load = [&](int j, const int8_t* from, int slot) __attribute__((always_inline)) {
-    if (ONCE && j >= kTokenLoads) direct_load16_once(from, off[j], lds + slot + 1024 * (j * W + wave));
+    if (ONCE && j >= kTokenLoads) direct_load16(Once(), from, off[j], lds + slot + 1024 * (j * W + wave));
     else direct_load16(from, off[j], lds + slot + 1024 * (j * W + wave));
   };
   // load j of stage k, which goes to `slot`; past the end of a row come zeros of the tokens (ask_end), anything of the channels

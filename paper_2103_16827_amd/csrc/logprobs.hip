@@ -255,7 +255,7 @@ struct Choice {
 
 // W waves a row or piece, R loads of 16 bytes a lane: up to 64 W R kPer logits.  W == 1: four rows a workgroup, a wave each.
 template <typename T, int W, int R>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W, W == 16 ? 8 : 1) void logprobs_kernel(LogprobParams p, Pieces c) {
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(LogprobParams p, Pieces c) {
   constexpr int N = kPer<T>, kRows = W == 1 ? 4 : 1;
   constexpr int kHolders = W == 1 ? 32 : 128;          // threads whose logits fit the LDS at once
   __shared__ float part[kRows][3 * W];

@@ -36,13 +36,14 @@ __device__ __forceinline__ void direct_load16(const void* base, uint32_t off, co
                :: "v"(off), "s"(base), "s"(m0v) : "memory");
 }
 // the same of bytes that nothing asks for again: past the 256 MB cache behind the L2s
-__device__ __forceinline__ void direct_load16_once(const void* gptr, const unsigned char* lds_wave_base) {
+struct Once {};
+__device__ __forceinline__ void direct_load16(Once, const void* gptr, const unsigned char* lds_wave_base) {
   const uint32_t m0v = __builtin_amdgcn_readfirstlane(
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)lds_wave_base);
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt"
                :: "v"(gptr), "s"(m0v) : "memory");
 }
-__device__ __forceinline__ void direct_load16_once(const void* base, uint32_t off, const unsigned char* lds_wave_base) {
+__device__ __forceinline__ void direct_load16(Once, const void* base, uint32_t off, const unsigned char* lds_wave_base) {
   const uint32_t m0v = __builtin_amdgcn_readfirstlane(
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)lds_wave_base);
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"

@@ -48,6 +48,20 @@ def test_linear_descriptors(kw, status):
     assert experts(d) == status
 
 
+@pytest.mark.parametrize("kw", [dict(M=(1 << 30) + 1), dict(N=(1 << 30) + 1), dict(N=(1 << 31) - 1, K=1), dict(M=(1 << 31) - 1, K=1), dict(M=1 << 20, N=1 << 20)])
+def test_linear_sides(kw):
+    d = desc(**kw)
+    assert linear(d) == SHAPE
+    assert dynamic(d, nbytes=1 << 20) == SHAPE
+    assert experts(d, rows=(1 << 31) - 1) == SHAPE
+
+
+def test_more_tiles_than_a_launch_counts():
+    assert experts(desc(M=100, N=1 << 29), 64) == SHAPE      # (a tile more for every group)
+    assert quantize(K=(1 << 30) + 1) == SHAPE
+    assert quantize(K=(1 << 31) - 1) == SHAPE
+
+
 def test_no_rows_are_no_work():
     d = desc(M=0)
     assert linear(d, None, None, None, None, None, None) == OK

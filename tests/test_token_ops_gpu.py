@@ -276,6 +276,21 @@ def test_experts_offsets_and_indexes_out_of_range():
         same(yd, want, f"offsets {offsets}")
 
 
+@pytest.mark.parametrize("E", [64, 65, 1000, 4096])
+def test_many_experts(E):
+    print(f"[case] {E} experts", flush=True)
+    g, N, K = gen(E), 20, 48
+    sizes = torch.randint(0, 3, (E,), generator=g)
+    sizes[E // 2] = 70
+    sizes[-1] = 1
+    offsets = np.concatenate([[0], np.cumsum(sizes.numpy())]).astype(np.int32)
+    M = int(offsets[-1])
+    x, xs, w, ws = codes(g, M, K), scales(g, M), codes(g, E, N, K), scales(g, E, N)
+    y = torch.full((M, N), float(FILL), device="cuda")
+    Q.experts_int8(x.cuda(), xs.cuda(), torch.from_numpy(offsets).cuda(), None, w.cuda(), ws.cuda(), None, y)
+    same(y, experts_ref(x, xs, offsets.tolist(), None, w, ws, None, torch.empty(M, N)), "experts")
+
+
 @pytest.mark.parametrize("sizes,rows", [([1] * 5 + [0] * 10 + [3], 1), ([9, 0, 16, 2] * 4, 20), ([40, 64, 1, 0] * 4, 33), ([128, 100, 70, 128] * 4, 70),
                                         ([300, 0, 17, 256] * 4, 300)])
 def test_experts_larger_than_the_cache(sizes, rows):

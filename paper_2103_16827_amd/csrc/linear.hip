@@ -31,25 +31,26 @@ constexpr int kLdsBytes = 160 * 1024;
 
 __device__ __align__(16) const uint8_t kZeros[16] = {};   // what stands for codes past the end of a row
 
-// Bytes [k, k + 16) of a row of K bytes, zeros past its end; any alignment.  A row's last bytes are loaded with those before
-// them and shifted down (byte by byte they would be a chain of up to 15 round trips to memory).
-__device__ __forceinline__ v4i row_chunk(const int8_t* row, int k, int K) {
-  if (k + 16 <= K) return *reinterpret_cast<const unaligned_chunk16*>(row + k);
-  v4i v = (v4i){0, 0, 0, 0};
-  if (k >= K) return v;
-  if (K < 16) {
-    for (int i = 0; k + i < K; ++i) v[i >> 2] |= (int)((uint32_t)(uint8_t)row[k + i] << (8 * (i & 3)));
-    return v;
-  }
-  const v4i all = *reinterpret_cast<const unaligned_chunk16*>(row + K - 16);
-  const int by = k + 16 - K, words = by >> 2;              // 1 .. 15 bytes
-  uint32_t w[5];
+// Rows that begin anywhere or end inside a chunk: chunk k (bytes [k, k + 16), zeros past the end of the K bytes) is loaded from
+// chunk_at(k, K), no branch around the load, and moved down by what that lies ahead of k once it is there.  (Byte by byte a
+// row's end would be a chain of up to 15 round trips to memory.)  K >= 16.
+__device__ __forceinline__ int chunk_at(int k, int K) { return min(k, K - 16); }
+__device__ __forceinline__ v4i moved_down(v4i all, int by) {               // by 0 .. 16 bytes, without a branch
+  const uint32_t eight = -(by >> 3 & 1), four = -(by >> 2 & 1), none = (by >> 4) - 1;
+  uint32_t w[5] = {(uint32_t)all[0], (uint32_t)all[1], (uint32_t)all[2], (uint32_t)all[3], 0};
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    w[i] = (uint32_t)(words == 0 ? all[i] : words == 1 ? (i < 3 ? all[(i + 1) & 3] : 0) : words == 2 ? (i < 2 ? all[(i + 2) & 3] : 0) : (i < 1 ? all[3] : 0));
-  w[4] = 0;
+  for (int i = 0; i < 4; ++i) w[i] = ((i < 2 ? w[i + 2] : 0) & eight) | (w[i] & ~eight);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = ((w[i + 1] & four) | (w[i] & ~four)) & none;
+  v4i v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = (int)__builtin_amdgcn_alignbyte(w[i + 1], w[i], by & 3);
+  return v;
+}
+// ... of a row shorter than 16
+__device__ __forceinline__ v4i short_row(const int8_t* row, int k, int K) {
+  v4i v = (v4i){0, 0, 0, 0};
+  for (int i = 0; k + i < K; ++i) v[i >> 2] |= (int)((uint32_t)(uint8_t)row[k + i] << (8 * (i & 3)));
   return v;
 }
 
@@ -340,19 +341,43 @@ __global__ __launch_bounds__(64 * W) void linear_few_kernel(LinearParams L, Orde
     }
     wait_vm<0>();
   } else {
-    v4i next[kLoads];
-    auto fetch = [&](int i) __attribute__((always_inline)) {
+    constexpr int D = 2;                           // steps on their way
+    v4i next[D][kLoads];
+    auto k_of = [&](int i, int j) __attribute__((always_inline)) { return (wave + i * W) * STEP + 16 * chunk[j]; };
+    auto fetch = [&](int i, v4i (&to)[kLoads]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) next[j] = row_chunk(row[j], (wave + i * W) * STEP + 16 * chunk[j], L.K);
+      for (int j = 0; j < kLoads; ++j) to[j] = *reinterpret_cast<const unaligned_chunk16*>(row[j] + chunk_at(k_of(i, j), L.K));
     };
-    if (mine > 0) fetch(0);
-    for (int i = 0; i < mine; ++i) {
+    auto multiply = [&](int i, const v4i (&from)[kLoads]) __attribute__((always_inline)) {
+      const bool whole = (wave + i * W + 1) * STEP <= L.K;
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) *(v4i*)(ring + 1024 * j + 16 * lane) = next[j];
-      if (i + 1 < mine) fetch(i + 1);
+      for (int j = 0; j < kLoads; ++j)
+        *(v4i*)(ring + 1024 * j + 16 * lane) = whole ? from[j] : moved_down(from[j], min(16, max(0, k_of(i, j) + 16 - L.K)));
       __builtin_amdgcn_wave_barrier();
       products(ring, 0);
       __builtin_amdgcn_wave_barrier();
+    };
+    if (L.K < 16) {
+      if (mine > 0) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) next[0][j] = short_row(row[j], 16 * chunk[j], L.K);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) *(v4i*)(ring + 1024 * j + 16 * lane) = next[0][j];
+        __builtin_amdgcn_wave_barrier();
+        products(ring, 0);
+      }
+    } else {
+#pragma unroll
+      for (int d = 0; d < D; ++d)
+        if (d < mine) fetch(d, next[d]);
+      for (int i = 0; i < mine; i += D) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+          if (i + d >= mine) break;
+          multiply(i + d, next[d]);
+          if (i + d + D < mine) fetch(i + d + D, next[d]);
+        }
+      }
     }
   }
 
@@ -635,10 +660,10 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearParams 
   wait_vm<0>();
 }
 
-// The same tiles where rows begin anywhere or end inside a chunk: rows come through registers.
+// The same tiles where rows begin anywhere or end inside a chunk, of 16 codes and more: rows come through registers.
 template <int MT, int NT, int WM, int WN, typename T>
 __global__ __launch_bounds__(64 * WM * WN) void linear_rows_kernel(LinearParams L, Order o) {
-  constexpr int STEP = 128, P = products_of<T>(NT), RPL = 1024 / STEP, CPR = STEP / 16;
+  constexpr int STEP = 128, P = products_of<T>(NT), RPL = 1024 / STEP, CPR = STEP / 16, D = 2;
   constexpr int W = WM * WN, BM = 16 * MT * WM, BN = 16 * NT * WN, kStage = (BM + BN) * STEP;
   constexpr int kTokenLoads = BM / RPL / W, kLoads = kTokenLoads + BN / RPL / W;
   static_assert(BM % (RPL * W) == 0 && BN % (RPL * W) == 0 && RPL * W % 16 == 0, "see linear_tile_kernel");
@@ -659,46 +684,49 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_rows_kernel(LinearParams 
   }
   Scales<BM, BN, 64 * W> sc;
   sc.load(L, t);
-  // step k's rows are asked for two steps before their products, into registers by turns
-  v4i next[2][kLoads];
+  // Step k's rows are asked for D steps before their products, into registers by turns; past the last step they are asked for
+  // all the same, so that the compiler can count which are on their way.
+  v4i next[D][kLoads];
+  auto k_of = [&](int k, int j) __attribute__((always_inline)) { return k * STEP + 16 * (j < kTokenLoads ? token_chunk : channel_chunk); };
   auto fetch = [&](int k, v4i (&to)[kLoads]) __attribute__((always_inline)) {
-    if ((k + 1) * STEP <= L.K) {
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j)
-        to[j] = *reinterpret_cast<const unaligned_chunk16*>(row[j] + k * STEP + 16 * (j < kTokenLoads ? token_chunk : channel_chunk));
-    } else if (k < steps) {
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) to[j] = row_chunk(row[j], k * STEP + 16 * (j < kTokenLoads ? token_chunk : channel_chunk), L.K);
-    }
+    for (int j = 0; j < kLoads; ++j) to[j] = *reinterpret_cast<const unaligned_chunk16*>(row[j] + chunk_at(k_of(k, j), L.K));
   };
-  auto put = [&](unsigned char* stage, const v4i (&from)[kLoads]) __attribute__((always_inline)) {
+  auto put = [&](int k, const v4i (&from)[kLoads]) __attribute__((always_inline)) {
+    unsigned char* stage = lds + (k & 1) * kStage;
+    const bool whole = (k + 1) * STEP <= L.K;
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) *(v4i*)(stage + 1024 * (j * W + wave) + 16 * lane) = from[j];
+    for (int j = 0; j < kLoads; ++j)
+      *(v4i*)(stage + 1024 * (j * W + wave) + 16 * lane) = whole ? from[j] : moved_down(from[j], min(16, max(0, k_of(k, j) + 16 - L.K)));
   };
   Sums<MT, NT> acc;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = (v4i){0, 0, 0, 0};
-  auto step = [&](int k, v4i (&free)[kLoads], const v4i (&ready)[kLoads]) __attribute__((always_inline)) {
-    const unsigned char* stage = lds + (k & 1) * kStage;
-    fetch(k + 2, free);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int at = 16 * ((4 * h + g) ^ swizzle<STEP>(r));
-      products_of_half<MT, NT, P, STEP>(acc, stage + (16 * MT * wm + r) * STEP + at, stage + (BM + 16 * NT * wn + channel_of<P>(0, r)) * STEP + at);
-    }
-    if (k + 1 < steps) put(lds + ((k + 1) & 1) * kStage, ready);
-    __syncthreads();
-  };
-  fetch(0, next[0]);
-  fetch(1, next[1]);
-  put(lds, next[0]);
+  for (int d = 0; d < D; ++d) fetch(d, next[d]);
+  put(0, next[0]);
   sc.put(scales);
-  __syncthreads();
-  for (int k = 0; k < steps; k += 2) {
-    step(k, next[0], next[1]);
-    if (k + 1 < steps) step(k + 1, next[1], next[0]);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  for (int k0 = 0;; k0 += D) {
+    bool more = true;
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      if (!more) continue;
+      const int k = k0 + d;
+      const unsigned char* stage = lds + (k & 1) * kStage;
+      fetch(k + D, next[d]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = 16 * ((4 * h + g) ^ swizzle<STEP>(r));
+        products_of_half<MT, NT, P, STEP>(acc, stage + (16 * MT * wm + r) * STEP + at, stage + (BM + 16 * NT * wn + channel_of<P>(0, r)) * STEP + at);
+      }
+      more = k + 1 < steps;
+      if (more) put(k + 1, next[(d + 1) % D]);
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    if (!more) break;
   }
   store_tile<MT, NT, BM, BN, 2 * kStage / W, T>(L, t, scales, lds + 2 * kStage / W * wave, 16 * MT * wm, 16 * NT * wn, acc);
 }
@@ -794,23 +822,27 @@ constexpr Form kForms[] = {
     {128, 256, 1, 3.39, 0.48, 0.556, 0.907},
     {256, 256, 1, 3.11, 1.71, 1.216, 1.216},
 };
-// ... where rows begin anywhere or end inside a chunk (14 shapes, of which the rule takes the fastest form but for 4 to 9 % in three)
+// ... where rows begin anywhere or end inside a chunk (20 shapes: rms 7 to 12 %, the rule takes the fastest form or one within 2 % for 16 of
+// them, within 6 % for three more and 12 % for the last)
 constexpr Form kRowForms[] = {
-    {16, 16, 4, 0.3, 2.0, 0.15, 0.16},         // linear_few, 8 waves
-    {16, 16, 8, 0.3, 1.5, 0.2, 0.108},         // 4 waves
-    {64, 128, 3, 2.0, 1.4, 0.95, 0.64},        // linear_rows, from here
-    {128, 256, 1, 4.0, 0.5, 1.5, 1.8},
+    {16, 16, 4, 0.65, 1.43, 0.116, 0.087},     // linear_few, 8 waves
+    {16, 32, 6, 0.31, 1.33, 0.204, 0.142},     // 4 waves
+    {32, 32, 5, 0.73, 1.58, 0.250, 0.173},
+    {64, 64, 4, 0.96, 1.21, 0.539, 0.406},     // linear_rows, from here
+    {64, 128, 3, 1.74, 1.23, 0.702, 0.604},
+    {128, 256, 1, 3.72, 1.24, 1.355, 1.862},
 };
+constexpr int kRowFormCount = sizeof(kRowForms) / sizeof(kRowForms[0]), kShortRowForms = 3;      // (linear_rows: K >= 16)
 constexpr double kBytesPerUs = 5.3e6;           // of memory
 
 template <int N>
-int fastest_form(const LinearParams& p, const Form (&forms)[N]) {
+int fastest_form(const LinearParams& p, const Form (&forms)[N], int among) {
   const double steps = (p.K + 127) / 128, units = compute_units();
   const double groups = groups_of(p), rows = p.M / groups;
   const double memory = (groups * p.N * p.K + (double)p.M * (p.K + 2.0 * p.N)) / kBytesPerUs;
   int best = 0;
   double least = 0;
-  for (int i = 0; i < N; ++i) {
+  for (int i = 0; i < among; ++i) {
     const Form& f = forms[i];
     const double in_group = !p.offsets ? std::ceil(rows / f.BM) : rows <= f.BM / 2 ? 1.0 : rows / f.BM + 0.5;
     const double load = groups * in_group * ((p.N + f.BN - 1) / f.BN) / units, group = p.offsets ? f.group : 0.0;
@@ -828,14 +860,16 @@ int fastest_form(const LinearParams& p, const Form (&forms)[N]) {
 template <typename T>
 hipError_t launch_typed(const LinearParams& p, hipStream_t st) {
   if (!direct_ok(p)) {
-    switch (fastest_form(p, kRowForms)) {
+    switch (fastest_form(p, kRowForms, p.K < 16 ? kShortRowForms : kRowFormCount)) {
       case 0: return launch_few<1, 1, 8, 1, false, int8_t, T>(p, st);
-      case 1: return launch_few<1, 1, 4, 1, false, int8_t, T>(p, st);
-      case 2: return launch_rows<2, 4, 2, 2, T>(p, st);
+      case 1: return launch_few<1, 2, 4, 1, false, int8_t, T>(p, st);
+      case 2: return launch_few<2, 2, 4, 1, false, int8_t, T>(p, st);
+      case 3: return launch_rows<1, 4, 4, 1, T>(p, st);
+      case 4: return launch_rows<2, 4, 2, 2, T>(p, st);
       default: return launch_rows<4, 4, 2, 4, T>(p, st);
     }
   }
-  switch (fastest_form(p, kForms)) {
+  switch (fastest_form(p, kForms, sizeof(kForms) / sizeof(kForms[0]))) {
     case 0: return launch_few<1, 1, 4, 2, true, int8_t, T>(p, st);
     case 1: return launch_few<1, 2, 4, 2, true, int8_t, T>(p, st);
     case 2: return launch_few<1, 4, 4, 1, true, int8_t, T>(p, st);

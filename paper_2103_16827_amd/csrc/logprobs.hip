@@ -471,7 +471,8 @@ __global__ __launch_bounds__(256) void logprobs_small_kernel(LogprobParams p) {
   const float ninf = -__builtin_inff();
   const float x = id < p.V ? to_float(((const T*)p.x + row * p.xs)[id]) : ninf;
   Ahead ahead;
-  ahead.load<T>(p, row, id);
+  ahead.ask(p, row, id);
+  ahead.x = __shfl(x, lane - id + min(max(ahead.tok, 0), p.V - 1));      // (the row is in its lanes)
   const float m = row_reduce<G>(x, [](float a, float b) { return fmaxf(a, b); });
   const float base = m == ninf ? 0.0f : m, d = x - base, e = __expf(d);
   const float s = row_reduce<G>(e, [](float a, float b) { return a + b; });

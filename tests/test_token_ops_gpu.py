@@ -143,6 +143,12 @@ def test_linear(M, N, K):
         yp.check()
 
 
+@pytest.mark.parametrize("M,N,K", [(1, 700, 2), (40, 50, 15), (700, 600, 5), (3000, 900, 9), (600, 500, 17), (1300, 700, 31), (200, 3000, 129), (777, 1029, 515), (2050, 1030, 127),
+                                   (1500, 1500, 400), (60, 5003, 1003), (33, 520, 4097), (1, 2001, 3001)])
+def test_linear_rows_of_any_alignment(M, N, K):
+    test_linear(M, N, K)
+
+
 @pytest.mark.parametrize("M,N,K", [(2, 17, 131071), (40, 16, 131056), (300, 256, 131056), (300, 300, 131071)])
 def test_linear_longest_sums(M, N, K):
     """Every product 128 x 128: the largest sums the accumulator is promised to hold, of either sign."""

@@ -2,15 +2,23 @@
 //   y[m,n] = ((float)(sum_k x[m,k] w[n,k]) x_scale[m]) w_scale[n] + bias[n].
 //
 // Both operands are rows of K consecutive codes, which is what v_mfma_i32_16x16x64_i8 wants: lane 16 g + r brings 16
-// consecutive codes of row r (chunk g of 64).  Rows go to LDS by direct loads (1 KiB each) in steps of 64 or 128 codes; the
+// consecutive codes of row r (chunk g of 64).  Rows go to LDS by direct loads (1 KiB each) in steps of 128 codes, whole cache lines; the
 // lane of a load that writes slot s of a row brings chunk s ^ f(row), so that the 16-byte reads of an operand (one chunk of
 // many rows) touch every bank once.  Weights are the first operand: a lane ends up with four consecutive channels of one
 // token, and which channels the rows of an operand are is chosen so that a lane has 16 bytes of y over one or two products.
 //
 // linear_few (few tokens): the weights pass once from memory to one workgroup, which is all such a product costs.  The waves
 // of a workgroup split K, each with a ring of its own in LDS and no barrier before the end, where the exact int32
-// partial sums meet in LDS.
-// linear_tile (more): tiles of BM x BN through a ring in LDS that the waves share, a barrier per step.
+// partial sums meet in LDS.  Bound by memory, and below 16 MB of weights by one launch and its chain of loads: 1 token of 4096 x 4096
+// 5.4 us, 32 of 11008 x 4096 10.7 with the weights in the 256 MB cache, 15.6 from memory (2.9 TB/s), 1 of 32768 x 4096 21 (6.3 TB/s).
+// linear_tile (more): tiles of BM x BN through a ring in LDS that the waves share, a barrier per step.  8192 x 14336 x 4096 355 us =
+// 2.7 POP/s, 8192^3 384 = 2.9: matrix pipes 62 % busy at the 1.9 GHz that the operands' power leaves (zeros instead of codes: 9 %
+// faster).  A step of a 256 x 256 tile keeps the LDS port (192 KiB read, 64 written, 128 bytes a cycle) as long as the products keep the
+// pipes.  Four waves of 128 x 128 each instead of eight of 128 x 64, which read a third less, have one wave per SIMD and were 3 to 6 % slower;
+// stages of 64 codes, three of them, too, at half the vector cache's rate; tiles in turn with the results of one leaving under the
+// products of the next spilled registers.
+// linear_rows: the same tiles for rows of any alignment, through registers.  777 x 1029 x 1003 7.8 us, 2000 x 2001 x 2001 24.5
+// (0.66 POP/s): its chain of loads, two steps ahead.
 #include "floats.hpp"
 #include "kernels.hpp"
 #include "lanes.hpp"
@@ -142,10 +150,9 @@ __device__ __forceinline__ int x_row(const LinearParams& L, int m) {
   return i >= 0 && i < L.x_rows ? i : -1;
 }
 
-// Slot of a row's chunk c is c ^ f: what eight consecutive lanes read of as many rows then lies in different banks.  A row of
-// 128 codes fills the banks, of 64 half of them.  Rows are counted as an operand's lanes read them (r = lane & 15).
-template <int STEP>
-__device__ __forceinline__ int swizzle(int r) { return STEP == 128 ? r & 7 : (r >> 1) & 3; }
+// Slot of a row's chunk c is c ^ f: what eight consecutive lanes read of as many rows then lies in different banks, which a row
+// of 128 codes fills.  Rows are counted as an operand's lanes read them (r = lane & 15).
+__device__ __forceinline__ int swizzle(int r) { return r & 7; }
 
 // Row r of product nt of a wave is its channel channel_of: lanes 16 g .. end with 4 P consecutive channels of a token over P
 // products, 16 bytes of y.
@@ -210,12 +217,12 @@ __global__ __launch_bounds__(64 * W) void linear_few_kernel(LinearParams L, Orde
     if (8 * j < TOKENS) {
       const int xr = x_row(L, t.lo + min(i, rows - 1));
       row[j] = L.x + (int64_t)max(xr, 0) * L.xs;
-      chunk[j] = (lane & 7) ^ swizzle<STEP>(i & 15);
+      chunk[j] = (lane & 7) ^ swizzle(i & 15);
       brings[j] = i < rows || i % 8 == 0;
     } else {
       const int n = i - TOKENS;
       row[j] = L.w + t.e * L.wes + (int64_t)min(t.n0 + n, L.N - 1) * L.ws;
-      chunk[j] = (lane & 7) ^ swizzle<STEP>(row_of<P>(n));
+      chunk[j] = (lane & 7) ^ swizzle(row_of<P>(n));
       brings[j] = true;
     }
   }
@@ -249,7 +256,7 @@ __global__ __launch_bounds__(64 * W) void linear_few_kernel(LinearParams L, Orde
   auto products = [&](const unsigned char* stage, int k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int at = 16 * ((4 * h + g) ^ swizzle<STEP>(r));
+      const int at = 16 * ((4 * h + g) ^ swizzle(r));
       v4i a[MT], b[NT];
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
@@ -526,7 +533,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearParams 
 
   // the rows that this lane brings, by 32-bit offsets from the tile's first rows (the launch sees to it that these do)
   const int first = RPL * wave + lane / CPR;
-  const int token_chunk = (lane % CPR) ^ swizzle<STEP>(first & 15), channel_chunk = (lane % CPR) ^ swizzle<STEP>(row_of<P>(first));
+  const int token_chunk = (lane % CPR) ^ swizzle(first & 15), channel_chunk = (lane % CPR) ^ swizzle(row_of<P>(first));
   const int8_t* xbase = L.x + (L.index ? 0 : (int64_t)t.lo * L.xs);
   const int8_t* wbase = L.w + t.e * L.wes + (int64_t)t.n0 * L.ws;
   uint32_t off[kLoads];
@@ -557,7 +564,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearParams 
   // half's are on their way into registers, and the next stage has come, the stage's room is free: it is asked for again there.
   Sums<MT, NT> acc;
   v4i a[MT], b[2][NT];
-  const int at[2] = {16 * (g ^ swizzle<STEP>(r)), 16 * ((4 + g) ^ swizzle<STEP>(r))};
+  const int at[2] = {16 * (g ^ swizzle(r)), 16 * ((4 + g) ^ swizzle(r))};
   const unsigned char* as = lds + (16 * MT * wm + r) * STEP;
   const unsigned char* bs = lds + (BM + 16 * NT * wn + channel_of<P>(0, r)) * STEP;
   auto read_a = [&](int mt, int slot, int h) __attribute__((always_inline)) { a[mt] = *(const v4i*)(as + slot + at[h] + 16 * mt * STEP); };
@@ -674,7 +681,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_rows_kernel(LinearParams 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
   const int wm = wave / WN, wn = wave % WN, steps = (L.K + STEP - 1) / STEP;
   const int first = RPL * wave + lane / CPR;
-  const int token_chunk = (lane % CPR) ^ swizzle<STEP>(first & 15), channel_chunk = (lane % CPR) ^ swizzle<STEP>(row_of<P>(first));
+  const int token_chunk = (lane % CPR) ^ swizzle(first & 15), channel_chunk = (lane % CPR) ^ swizzle(row_of<P>(first));
   const int8_t* row[kLoads];
 #pragma unroll
   for (int j = 0; j < kLoads; ++j) {
@@ -719,7 +726,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_rows_kernel(LinearParams 
       fetch(k + D, next[d]);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int at = 16 * ((4 * h + g) ^ swizzle<STEP>(r));
+        const int at = 16 * ((4 * h + g) ^ swizzle(r));
         products_of_half<MT, NT, P, STEP>(acc, stage + (16 * MT * wm + r) * STEP + at, stage + (BM + 16 * NT * wn + channel_of<P>(0, r)) * STEP + at);
       }
       more = k + 1 < steps;

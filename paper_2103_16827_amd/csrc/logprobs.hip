@@ -7,11 +7,16 @@
 //   - the alternatives by a threshold.  Threads are columns, 64 of them or four times as many (some threads each): the `top`-th
 //     largest of the columns' maxima is reached by `top` logits at least, and hardly more where the best are spread by
 //     chance.  The few threads whose maximum reaches it put their logits in LDS, where all threads look for those
-//     that do; these are ranked by counting.  Where they are too many for the room (thousands of equal logits), the best are
-//     taken out one after the other, from memory.
+//     that do; these are ranked by counting.  Where they are too many for the room, most often because the best end among equal
+//     logits (a mask of -infinity or of the type's lowest value that leaves fewer than `top`), the larger ones are taken, and of the
+//     equal ones those up to a limit on their ids, found in the same way.  Where these are too many as well (hundreds of
+//     unequal logits in few columns), the best are taken out one after the other, from memory.
 // Pieces leave (m, s, t) and their best in the workspace; a second kernel joins them.
 // What bounds it: the logits' way from memory, and next to it about eleven vector operations per logit, of which the
-// exponential takes four times the others' time.
+// exponential takes four times the others' time.  4096 rows of 50257 bf16 logits 73 us (5.6 TB/s), with 5 alternatives 79, with 20 81;
+// 64 of 151936 fp16 11.3 and 15.0; 1 of 128256 float32 5.4 and 10.4, of which a launch and its first loads are half, the second
+// kernel another half.  With 3 logits left of 50257 and 20 alternatives, 512 rows take 42 us for 19 (657 when they were taken out one
+// after the other).
 #include "floats.hpp"
 #include "kernels.hpp"
 #include "lanes.hpp"
@@ -596,8 +601,9 @@ constexpr int kWhole = 16 * 64 * 8 * 16, kPiece = 8 * 64 * 13 * 16;
 
 // A row that one workgroup can take is one piece: it is done before a second kernel would begin (32000 float32 logits and five
 // alternatives 6.7 us, 9.9 in 15 pieces; 1000 such rows 26.5, 33.4 in two).  Few long rows: pieces for the whole chip, of 8 KiB and
-// more, whose best the workgroup that joins them can hold.  Else the number of them that leaves the busiest compute unit the least to do, up to twice as many as it takes (128 rows
-// of 128256 fp16 logits with 20 alternatives 20.1 us in 4 pieces, 20.9 in 2, 22.4 in 3; 1000 of 100000 49.4 in 2, 52.4 in 3, 54.7 in 4).
+// more, whose best the workgroup that joins them can hold.  Else the number of them that leaves the busiest compute unit the least
+// to do, up to twice as many as it takes (128 rows of 128256 fp16 logits with 20 alternatives 20.1 us in 4 pieces, 20.9 in 2, 22.4 in
+// 3; 1000 of 100000 49.4 in 2, 52.4 in 3, 54.7 in 4).
 Pieces pieces_of(int64_t rows, int V, int bytes, int top) {
   Pieces c{};
   const int64_t all = (int64_t)V * bytes;
@@ -650,6 +656,9 @@ hipError_t launch_logprobs(const LogprobParams& p, int x_type, void* workspace, 
       return launch_kernel(G == 16 ? logprobs_small_kernel<T, 16> : G == 32 ? logprobs_small_kernel<T, 32> : logprobs_small_kernel<T, 64>,
                            dim3(g.x, g.y), dim3(256), 0, st, p);
     }
+    // As many registers as a row needs and as few waves as then hold it: rows meet fewer barriers, and more of them share a unit.
+    // (4096 rows of 50257 bf16 logits and 20 alternatives: 8 waves of 13 loads 82 us, 16 of 8 99; of 18000: 4 of 10 37 us, 8 of 8 48, but
+    // where there are few rows, 16 of 20000, 7.6 us against 6.9)
     if (loads <= 64) e = launch(logprobs_kernel<T, 1, 1>, 1);
     else if (loads <= 256) e = launch(logprobs_kernel<T, 1, 4>, 1);
     else if (loads <= 512) e = launch(logprobs_kernel<T, 4, 2>, 4);

@@ -893,7 +893,7 @@ hipError_t launch_typed(const LinearParams& p, hipStream_t st) {
 }  // namespace
 
 // Few enough floats for every workgroup to quantise them: with kFloats over all rounds of workgroups on the chip it takes
-// less than the launch that it saves.
+// less than the launch that it saves (one token of 2048 x 2048: 6.7 us a call, 10.0 as two kernels).
 bool linear_takes_floats(const LinearParams& p, int x_type) {
   const int64_t size = x_type == 0 ? 4 : 2, all = (int64_t)p.M * p.K;
   LinearParams codes = p;                // as if tokens were codes on a boundary: the weights are what is asked about

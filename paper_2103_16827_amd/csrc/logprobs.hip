@@ -447,8 +447,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
   if (c.n > 1 && tid >= top && tid < p.top) c.best[unit * p.top + tid] = 0;
 }
 
-// Rows of up to G = 16, 32 or 64 logits: a lane each, 64 / G rows a wave.  Reductions by exchanges within the row's lanes; the
-// alternatives one after the other, or their ranks by comparing every logit with all.
+// Rows of up to 4 G = 16, 32 or 64 logits: G lanes of four logits each (l, G + l, ..), 64 / G rows a wave.  Reductions by exchanges
+// within 16 lanes; the alternatives one after the other, or their ranks by comparing every logit with all.  Bound by the instructions:
+// 25600 rows of 29 float32 logits and 3 alternatives 4.5 us, with a lane for every logit and two to eight times the exchanges 6.5.
 template <int G, typename V, typename Op>
 __device__ __forceinline__ V row_reduce(V v, Op op) {
   auto moved = [&](auto ctrl) __attribute__((always_inline)) {
@@ -459,56 +460,76 @@ __device__ __forceinline__ V row_reduce(V v, Op op) {
   using std::integral_constant;
   v = op(v, moved(integral_constant<int, 0xb1>()));    // neighbours, pairs, halves of eight, of sixteen
   v = op(v, moved(integral_constant<int, 0x4e>()));
-  v = op(v, moved(integral_constant<int, 0x141>()));
-  v = op(v, moved(integral_constant<int, 0x140>()));
-  if constexpr (G >= 32) v = op(v, __shfl_xor(v, 16));
-  if constexpr (G >= 64) v = op(v, __shfl_xor(v, 32));
+  if constexpr (G >= 8) v = op(v, moved(integral_constant<int, 0x141>()));
+  if constexpr (G >= 16) v = op(v, moved(integral_constant<int, 0x140>()));
   return v;
 }
 
 template <typename T, int G>
 __global__ __launch_bounds__(256) void logprobs_small_kernel(LogprobParams p) {
-  constexpr int kRows = 64 / G;
-  __shared__ __align__(16) uint32_t orders[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, id = lane % G;
+  constexpr int kRows = 64 / G, B = 4;
+  __shared__ __align__(16) uint32_t orders[4][64 * B];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane % G;
   const int64_t row = ((((int64_t)blockIdx.y << kGridShift) + blockIdx.x) * 4 + wave) * kRows + lane / G;
   if (row >= p.rows) return;                           // (no barriers below)
   const float ninf = -__builtin_inff();
-  const float x = id < p.V ? to_float(((const T*)p.x + row * p.xs)[id]) : ninf;
+  float x[B];
+#pragma unroll
+  for (int b = 0; b < B; ++b) x[b] = b * G + l < p.V ? to_float(((const T*)p.x + row * p.xs)[b * G + l]) : ninf;
   Ahead ahead;
-  ahead.ask(p, row, id);
-  ahead.x = __shfl(x, lane - id + min(max(ahead.tok, 0), p.V - 1));      // (the row is in its lanes)
-  const float m = row_reduce<G>(x, [](float a, float b) { return fmaxf(a, b); });
-  const float base = m == ninf ? 0.0f : m, d = x - base, e = __expf(d);
-  const float s = row_reduce<G>(e, [](float a, float b) { return a + b; });
-  const float t = row_reduce<G>(e * fmaxf(d, -1000.0f), [](float a, float b) { return a + b; });
+  ahead.load<T>(p, row, l);
+  const float m = row_reduce<G>(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), [](float a, float b) { return fmaxf(a, b); });
+  const float base = m == ninf ? 0.0f : m;
+  float s = 0.0f, t = 0.0f;
+#pragma unroll
+  for (int b = 0; b < B; ++b) {
+    const float d = x[b] - base, e = __expf(d);
+    s += e;
+    t = fmaf(e, fmaxf(d, -1000.0f), t);
+  }
+  s = row_reduce<G>(s, [](float a, float b) { return a + b; });
+  t = row_reduce<G>(t, [](float a, float b) { return a + b; });
   const Scorer score(m, s, t);
-  score.template tokens<T>(p, row, id, G, ahead);
+  score.template tokens<T>(p, row, l, G, ahead);
   if (p.top == 0) return;
-  const uint32_t own = id < p.V ? order_of(x) : 0;
+  if (score.bad) {
+    for (int j = l; j < p.top; j += G) score.alternative(p, row, j, 0);
+    return;
+  }
+  uint32_t own[B];                                     // 0: no logit, or taken
+#pragma unroll
+  for (int b = 0; b < B; ++b) own[b] = b * G + l < p.V ? order_of(x[b]) : 0;
   if (4 * p.top < p.V) {
-    // few: taken out one after the other, of equal ones the lowest (a lane's number is 0 once it was taken)
-    uint32_t left = own;
+    // few: taken out one after the other, of equal ones the lowest
     for (int j = 0; j < p.top; ++j) {
-      const uint32_t most = row_reduce<G>(left, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
-      const uint64_t at = __ballot(left == most && id < p.V) >> (lane / G * G);
-      if (id == __ffsll((unsigned long long)at) - 1) {
-        score.alternative(p, row, j, (uint64_t)own << 32 | (uint32_t)~id);
-        left = 0;
-      }
+      auto most_of = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
+      const uint32_t most = row_reduce<G>(most_of(most_of(own[0], own[1]), most_of(own[2], own[3])), most_of);
+      uint32_t id = ~0u;
+#pragma unroll
+      for (int b = B - 1; b >= 0; --b) id = own[b] == most ? b * G + l : id;
+      id = row_reduce<G>(id, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+      if (id % G == l) score.alternative(p, row, j, (uint64_t)most << 32 | ~id);
+#pragma unroll
+      for (int b = 0; b < B; ++b) own[b] = b * G + l == id ? 0 : own[b];
     }
     return;
   }
-  orders[wave][lane] = own;
-  sync<1>();
-  int rank = 0;
-#pragma unroll 2
-  for (int o = 0; o < p.V; o += 4) {                   // (lanes past the row hold 0)
-    const v4u c = *reinterpret_cast<const v4u*>(&orders[wave][lane / G * G + o]);
+  uint32_t* all = &orders[wave][lane / G * G * B];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) rank += c[k] > own || (c[k] == own && o + k < id);
+  for (int b = 0; b < B; ++b) all[b * G + l] = own[b];
+  sync<1>();
+  int rank[B] = {};
+#pragma unroll 2
+  for (int o = 0; o < p.V; o += 4) {                   // (past the row there are zeros)
+    const v4u c = *reinterpret_cast<const v4u*>(all + o);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int b = 0; b < B; ++b) rank[b] += c[k] > own[b] || (c[k] == own[b] && o + k < b * G + l);
   }
-  if (rank < p.top && id < p.V) score.alternative(p, row, rank, (uint64_t)own << 32 | (uint32_t)~id);
+#pragma unroll
+  for (int b = 0; b < B; ++b)
+    if (rank[b] < p.top && b * G + l < p.V) score.alternative(p, row, rank[b], (uint64_t)own[b] << 32 | (uint32_t)~(b * G + l));
 }
 
 // A workgroup joins the pieces of a row.
@@ -651,9 +672,9 @@ hipError_t launch_logprobs(const LogprobParams& p, int x_type, void* workspace, 
       return launch_kernel(kernel, dim3(g.x, g.y), dim3(waves == 1 ? 256 : 64 * waves), 0, st, p, c);
     };
     if (p.V <= 64) {
-      const int G = p.V <= 16 ? 16 : p.V <= 32 ? 32 : 64, rows = 4 * 64 / G;
+      const int G = p.V <= 16 ? 4 : p.V <= 32 ? 8 : 16, rows = 4 * 64 / G;
       const GridShape g = grid_shape((p.rows + rows - 1) / rows);
-      return launch_kernel(G == 16 ? logprobs_small_kernel<T, 16> : G == 32 ? logprobs_small_kernel<T, 32> : logprobs_small_kernel<T, 64>,
+      return launch_kernel(G == 4 ? logprobs_small_kernel<T, 4> : G == 8 ? logprobs_small_kernel<T, 8> : logprobs_small_kernel<T, 16>,
                            dim3(g.x, g.y), dim3(256), 0, st, p);
     }
     // As many registers as a row needs and as few waves as then hold it: rows meet fewer barriers, and more of them share a unit.

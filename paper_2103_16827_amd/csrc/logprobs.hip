@@ -447,9 +447,10 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
   if (c.n > 1 && tid >= top && tid < p.top) c.best[unit * p.top + tid] = 0;
 }
 
-// Rows of up to 4 G = 16, 32 or 64 logits: G lanes of four logits each (l, G + l, ..), 64 / G rows a wave.  Reductions by exchanges
-// within 16 lanes; the alternatives one after the other, or their ranks by comparing every logit with all.  Bound by the instructions:
-// 25600 rows of 29 float32 logits and 3 alternatives 4.5 us, with a lane for every logit and two to eight times the exchanges 6.5.
+// Rows of up to B G = 16, 32, 64, 128 or 256 logits: G lanes of B logits each (l, G + l, ..), 64 / G rows a wave.  Reductions by
+// exchanges within 16 lanes; the alternatives one after the other, or (B == 4) their ranks by comparing every logit with all.
+// Bound by the instructions: 25600 rows of 29 float32 logits and 3 alternatives 4.5 us, with a lane for every logit and two to
+// eight times the exchanges 6.5.
 template <int G, typename V, typename Op>
 __device__ __forceinline__ V row_reduce(V v, Op op) {
   auto moved = [&](auto ctrl) __attribute__((always_inline)) {
@@ -465,10 +466,10 @@ __device__ __forceinline__ V row_reduce(V v, Op op) {
   return v;
 }
 
-template <typename T, int G>
+template <typename T, int G, int B>
 __global__ __launch_bounds__(256) void logprobs_small_kernel(LogprobParams p) {
-  constexpr int kRows = 64 / G, B = 4;
-  __shared__ __align__(16) uint32_t orders[4][64 * B];
+  constexpr int kRows = 64 / G;
+  __shared__ __align__(16) uint32_t orders[4][B == 4 ? 64 * B : 4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane % G;
   const int64_t row = ((((int64_t)blockIdx.y << kGridShift) + blockIdx.x) * 4 + wave) * kRows + lane / G;
   if (row >= p.rows) return;                           // (no barriers below)
@@ -478,7 +479,10 @@ __global__ __launch_bounds__(256) void logprobs_small_kernel(LogprobParams p) {
   for (int b = 0; b < B; ++b) x[b] = b * G + l < p.V ? to_float(((const T*)p.x + row * p.xs)[b * G + l]) : ninf;
   Ahead ahead;
   ahead.load<T>(p, row, l);
-  const float m = row_reduce<G>(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), [](float a, float b) { return fmaxf(a, b); });
+  float m = x[0];
+#pragma unroll
+  for (int b = 1; b < B; ++b) m = fmaxf(m, x[b]);
+  m = row_reduce<G>(m, [](float a, float b) { return fmaxf(a, b); });
   const float base = m == ninf ? 0.0f : m;
   float s = 0.0f, t = 0.0f;
 #pragma unroll
@@ -499,11 +503,14 @@ __global__ __launch_bounds__(256) void logprobs_small_kernel(LogprobParams p) {
   uint32_t own[B];                                     // 0: no logit, or taken
 #pragma unroll
   for (int b = 0; b < B; ++b) own[b] = b * G + l < p.V ? order_of(x[b]) : 0;
-  if (4 * p.top < p.V) {
+  if (B > 4 || 4 * p.top < p.V) {
     // few: taken out one after the other, of equal ones the lowest
     for (int j = 0; j < p.top; ++j) {
       auto most_of = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
-      const uint32_t most = row_reduce<G>(most_of(most_of(own[0], own[1]), most_of(own[2], own[3])), most_of);
+      uint32_t most = own[0];
+#pragma unroll
+      for (int b = 1; b < B; ++b) most = most_of(most, own[b]);
+      most = row_reduce<G>(most, most_of);
       uint32_t id = ~0u;
 #pragma unroll
       for (int b = B - 1; b >= 0; --b) id = own[b] == most ? b * G + l : id;
@@ -514,22 +521,24 @@ __global__ __launch_bounds__(256) void logprobs_small_kernel(LogprobParams p) {
     }
     return;
   }
-  uint32_t* all = &orders[wave][lane / G * G * B];
+  if constexpr (B == 4) {
+    uint32_t* all = &orders[wave][lane / G * G * B];
 #pragma unroll
-  for (int b = 0; b < B; ++b) all[b * G + l] = own[b];
-  sync<1>();
-  int rank[B] = {};
+    for (int b = 0; b < B; ++b) all[b * G + l] = own[b];
+    sync<1>();
+    int rank[B] = {};
 #pragma unroll 2
-  for (int o = 0; o < p.V; o += 4) {                   // (past the row there are zeros)
-    const v4u c = *reinterpret_cast<const v4u*>(all + o);
+    for (int o = 0; o < p.V; o += 4) {                 // (past the row there are zeros)
+      const v4u c = *reinterpret_cast<const v4u*>(all + o);
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int b = 0; b < B; ++b) rank[b] += c[k] > own[b] || (c[k] == own[b] && o + k < b * G + l);
+        for (int b = 0; b < B; ++b) rank[b] += c[k] > own[b] || (c[k] == own[b] && o + k < b * G + l);
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+      if (rank[b] < p.top && b * G + l < p.V) score.alternative(p, row, rank[b], (uint64_t)own[b] << 32 | (uint32_t)~(b * G + l));
   }
-#pragma unroll
-  for (int b = 0; b < B; ++b)
-    if (rank[b] < p.top && b * G + l < p.V) score.alternative(p, row, rank[b], (uint64_t)own[b] << 32 | (uint32_t)~(b * G + l));
 }
 
 // A workgroup joins the pieces of a row.
@@ -671,10 +680,13 @@ hipError_t launch_logprobs(const LogprobParams& p, int x_type, void* workspace, 
       const GridShape g = grid_shape(waves == 1 ? (units + 3) / 4 : units);
       return launch_kernel(kernel, dim3(g.x, g.y), dim3(waves == 1 ? 256 : 64 * waves), 0, st, p, c);
     };
-    if (p.V <= 64) {
+    // (25600 rows of 128 float32 logits and 5 alternatives 9.2 us, a wave a row 21.7, 16 rows 3.7 and 4.7; 25600 of 256 bf16 and 8 alternatives
+    // 17.9 and 24.6, but 1000 rows 6.6 and 5.4)
+    if (p.V <= 64 || (p.V <= 128 && p.top <= 5) || (p.V <= 256 && p.top <= 8 && p.rows >= 4096)) {
       const int G = p.V <= 16 ? 4 : p.V <= 32 ? 8 : 16, rows = 4 * 64 / G;
       const GridShape g = grid_shape((p.rows + rows - 1) / rows);
-      return launch_kernel(G == 4 ? logprobs_small_kernel<T, 4> : G == 8 ? logprobs_small_kernel<T, 8> : logprobs_small_kernel<T, 16>,
+      return launch_kernel(G == 4 ? logprobs_small_kernel<T, 4, 4> : G == 8 ? logprobs_small_kernel<T, 8, 4> : p.V <= 64 ? logprobs_small_kernel<T, 16, 4>
+                           : p.V <= 128 ? logprobs_small_kernel<T, 16, 8> : logprobs_small_kernel<T, 16, 16>,
                            dim3(g.x, g.y), dim3(256), 0, st, p);
     }
     // As many registers as a row needs and as few waves as then hold it: rows meet fewer barriers, and more of them share a unit.

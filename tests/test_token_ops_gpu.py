@@ -506,6 +506,26 @@ def test_token_logprobs_pieces(rows, V, top):
     check_scores(x.float(), None, top)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V,top", [(16, 3), (17, 4), (33, 16), (64, 15), (65, 5), (128, 5), (129, 8), (200, 1), (256, 8), (256, 0), (257, 8)])
+def test_token_logprobs_many_short_rows(V, top, dtype):
+    print(f"[case] logprobs 4100 x {V} {dtype} top {top}", flush=True)
+    g = gen(V + top)
+    x = (torch.randn(4100, V, generator=g) * 3).to(dtype)
+    x[1] = 0.0
+    x[2] = float("-inf")
+    x[3] = torch.finfo(dtype).min
+    x[4, 2:] = float("-inf")
+    x[5, V // 2] = float("nan")
+    x[6, V - 1] = float("inf")
+    x[7] = torch.where(torch.arange(V) % 2 == 0, 0.0, -0.0).to(dtype)
+    x[8] = (torch.arange(V) % 3).to(dtype)
+    x[4099] = torch.arange(V).to(dtype)
+    tokens = torch.randint(-1, V + 1, (4100, 2), generator=g).int()
+    check_scores(x, tokens, top, Padded(4100, V, dtype, V + 3, 1, x))
+    check_scores(x[:9], None, top)
+
+
 def test_token_logprobs_rows_beyond_32_bits():
     print("[case] logprobs, offsets beyond 32 bits", flush=True)
     g = gen(12)

@@ -527,13 +527,13 @@ __global__ __launch_bounds__(256) void logprobs_small_kernel(LogprobParams p) {
     for (int b = 0; b < B; ++b) all[b * G + l] = own[b];
     sync<1>();
     int rank[B] = {};
-#pragma unroll 2
+#pragma unroll 1
     for (int o = 0; o < p.V; o += 4) {                 // (past the row there are zeros)
       const v4u c = *reinterpret_cast<const v4u*>(all + o);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int b = 0; b < B; ++b)
 #pragma unroll
-        for (int b = 0; b < B; ++b) rank[b] += c[k] > own[b] || (c[k] == own[b] && o + k < b * G + l);
+        for (int k = 0; k < 4; ++k) rank[b] += c[k] > own[b] - (uint32_t)(o + k < b * G + l);      // (an equal one before it is ahead)
     }
 #pragma unroll
     for (int b = 0; b < B; ++b)

@@ -124,7 +124,7 @@ __device__ __forceinline__ void sync() {
 // LDS of a choice of the best: the largest number in each column, and the candidates
 template <int W>
 struct Choice {
-  static constexpr int kQuarters = 4;                  // columns / 64, where `top` is large
+  static constexpr int kQuarters = 4;                  // columns / 64, where there are many (`wide`)
   __align__(16) uint32_t column[64 * kQuarters];
   uint64_t cand[kRoom];
   uint64_t wave_best[W];
@@ -139,14 +139,14 @@ struct Choice {
     if (tid == 0) count = holders = 0;
   }
   // own: the order of the thread's largest.  (A sync comes before it and after it.)
-  __device__ __forceinline__ void offer(int top, uint32_t own, int tid) {
-    atomicMax(&column[(tid & 63) + (top > 24 ? 64 * ((tid >> 6) % kQuarters) : 0)], own);
+  __device__ __forceinline__ void offer(bool wide, uint32_t own, int tid) {
+    atomicMax(&column[(tid & 63) + (wide ? 64 * ((tid >> 6) % kQuarters) : 0)], own);
   }
   // One wave: the largest number that at least n of the columns reach, 0 if there is none (where there are four times 64 in its bits from
   // `low` on).
-  __device__ __forceinline__ uint32_t limit(int top, int n, int low) const {
+  __device__ __forceinline__ uint32_t limit(bool wide, int n, int low) const {
     const int lane = threadIdx.x & 63;
-    if (top <= 24) {
+    if (!wide) {
       const uint32_t mine = column[lane];
       int above = 0;
 #pragma unroll 2
@@ -172,9 +172,9 @@ struct Choice {
   // leaves fewer than `top`): the larger ones, and of the equal ones those whose ids reach a limit found in the same way.  each(f)
   // calls f(order, ~id) for the thread's logits.  False if these are too many as well.  (A sync comes before it.)
   template <typename Each>
-  __device__ __forceinline__ bool among_equals(int top, int tid, Each&& each) {
+  __device__ __forceinline__ bool among_equals(bool wide, int top, int tid, Each&& each) {
     if (W == 1 || tid < 64) {
-      const uint32_t l = limit(top, top, 0);
+      const uint32_t l = limit(wide, top, 0);
       if ((tid & 63) == 0) least = l;
     }
     sync<W>();
@@ -186,12 +186,12 @@ struct Choice {
       if (order > value) add((uint64_t)order << 32 | id);
       else if (order == value) first = max(first, id);
     });
-    offer(top, first, tid);
+    offer(wide, first, tid);
     sync<W>();
     const int larger = count;
     if (larger > kRoom) return false;
     if (W == 1 || tid < 64) {
-      const uint32_t l = larger < top ? limit(top, top - larger, 0) : ~0u;
+      const uint32_t l = larger < top ? limit(wide, top - larger, 0) : ~0u;
       if ((tid & 63) == 0) least = l;
     }
     sync<W>();
@@ -318,8 +318,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
   sweep([&](float a, float b) { m = max3(m, a, b); });
   const uint32_t own = order_of(m);                    // of this thread's logits
   m = wave_max(m);
-  // (a wave on its own has too few threads for four times 64 columns: a lane's loads, or the words of its only one, are four)
-  const bool by_load = W == 1 && top > 24;
+  // Four times 64 columns for many alternatives, and for a wave on its own where few of its lanes hold logits; there a lane's loads,
+  // or the words of its only one, are four.
+  const bool by_load = W == 1 && (top > 24 || loads < 2 * top), wide = top > 24 || by_load;
   if (by_load) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -334,7 +335,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
       choice.column[64 * q + lane] = order_of(most);
     }
   } else if (top > 0) {
-    choice.offer(top, own, tid);
+    choice.offer(wide, own, tid);
   }
   if constexpr (W > 1) {
     if (lane == 0) part[0][wave] = m;
@@ -342,7 +343,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
   sync<W>();
   if constexpr (W > 1) m = wave_max(part[0][lane % W]);
   if (top > 0 && (W == 1 || wave == 0)) {              // (meanwhile the others go on)
-    const uint32_t l = choice.limit(top, top, 12);
+    const uint32_t l = choice.limit(wide, top, 12);
     if (lane == 0) choice.least = l;
   }
   const float base = m == ninf ? 0.0f : m;             // (nothing but -infinity: every exponential is 0)
@@ -441,7 +442,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logprobs_kernel(Logprob
     sync<W>();
     fits = choice.count <= kRoom;
   }
-  if (!fits) fits = choice.among_equals(top, tid, each);
+  if (!fits) fits = choice.among_equals(wide, top, tid, each);
   if (fits) choice.rank(top, tid, leave);
   else choice.one_by_one(top, len, tid, [&](int i) { return key_of(to_float(x[i]), v0 + i); }, leave);
   if (c.n > 1 && tid >= top && tid < p.top) c.best[unit * p.top + tid] = 0;
@@ -603,10 +604,11 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(LogprobParams p, 
   uint64_t own = 0;
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) own = held[i] > own ? held[i] : own;
-  choice.offer(p.top, (uint32_t)(own >> 32), tid);
+  const bool wide = p.top > 24;
+  choice.offer(wide, (uint32_t)(own >> 32), tid);
   sync<W>();
   // (where fewer columns than that have a key the limit is 0 and every key is a candidate)
-  const uint32_t limit = choice.limit(p.top, p.top, 12);
+  const uint32_t limit = choice.limit(wide, p.top, 12);
   if ((uint32_t)(own >> 32) >= limit) {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
@@ -615,7 +617,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(LogprobParams p, 
   sync<W>();
   bool fits = choice.count <= kRoom;
   if (!fits)
-    fits = choice.among_equals(p.top, tid, [&](auto&& f) __attribute__((always_inline)) {
+    fits = choice.among_equals(wide, p.top, tid, [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < kHeld; ++i)
         if (held[i] != 0) f((uint32_t)(held[i] >> 32), (uint32_t)held[i]);

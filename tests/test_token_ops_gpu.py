@@ -526,6 +526,19 @@ def test_token_logprobs_many_short_rows(V, top, dtype):
     check_scores(x[:9], None, top)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V,top", [(65, 24), (66, 9), (100, 16), (129, 24), (190, 24), (250, 16), (300, 24)])
+def test_token_logprobs_rows_of_few_lanes(V, top, dtype):
+    print(f"[case] logprobs {V} {dtype} top {top}", flush=True)
+    g = gen(V + top)
+    x = (torch.randn(70, V, generator=g) * 3).to(dtype)
+    x[1] = 1.0
+    x[2, 5:] = float("-inf")
+    x[3, ::2] = torch.finfo(dtype).min
+    x[4] = torch.arange(V).to(dtype)
+    check_scores(x, torch.randint(0, V, (70, 1), generator=g).int(), top, Padded(70, V, dtype, V + 5, 3, x))
+
+
 def test_token_logprobs_rows_beyond_32_bits():
     print("[case] logprobs, offsets beyond 32 bits", flush=True)
     g = gen(12)

@@ -433,8 +433,13 @@ def _on_device(x, *others):
     return stream
 
 
-def _bytes(t):
-    return 0 if t is None else t.numel() * t.element_size()
+def _room(t):
+    """The bytes that a workspace has for a kernel: of one that repeats or skips elements, its element count says nothing."""
+    if t is None:
+        return 0
+    if not t.is_contiguous():
+        _refuse("workspace", t, "a dense tensor")
+    return t.numel() * t.element_size()
 
 
 def quantize_tokens(x, q, scale):
@@ -475,10 +480,10 @@ def linear_int8_dynamic(x, w, w_scale, bias, y, workspace):
     """qasr_linear_int8_dynamic: float x [M, K], quantised token by token in the workspace, through codes w [N, K] -> float y."""
     (M, K), N = x.shape, w.shape[0]
     kind = _float_type(x, "x")
-    d = _linear_desc(M, N, K, _rows(x, (M, K), "x"), w, w_scale, bias, y)
+    d, room = _linear_desc(M, N, K, _rows(x, (M, K), "x"), w, w_scale, bias, y), _room(workspace)
     stream = _on_device(x, w, w_scale, bias, y, workspace)
     _check(lib().qasr_linear_int8_dynamic(ctypes.byref(d), x.data_ptr(), kind, w.data_ptr(), w_scale.data_ptr(), _ptr(bias),
-                                          y.data_ptr(), _ptr(workspace), _bytes(workspace), stream), "qasr_linear_int8_dynamic")
+                                          y.data_ptr(), _ptr(workspace), room, stream), "qasr_linear_int8_dynamic")
     return y
 
 
@@ -531,9 +536,10 @@ def token_logprobs(x, tokens=None, logprob=None, entropy=None, top_ids=None, top
             raise ValueError("top_ids and top_logprob go together")
         _dense(top_ids, _int32, (rows, top), "top_ids")
         _dense(top_logprob, _f32, (rows, top), "top_logprob")
+    room = _room(workspace)
     stream = _on_device(x, tokens, logprob, entropy, top_ids, top_logprob, workspace)
     _check(lib().qasr_token_logprobs(x.data_ptr(), kind, rows, V, xs, _ptr(tokens), n, _ptr(logprob), _ptr(entropy), top,
-                                     _ptr(top_ids), _ptr(top_logprob), _ptr(workspace), _bytes(workspace), stream),
+                                     _ptr(top_ids), _ptr(top_logprob), _ptr(workspace), room, stream),
            "qasr_token_logprobs")
 
 

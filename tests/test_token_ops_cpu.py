@@ -171,3 +171,14 @@ def test_binding_holds_tensors_against_the_call():
                  (lg, None, None, None, tok, f32(4, 2)), (lg[:, ::2], tok, f32(4, 1)), (lg, tok, f32(4, 1))]:
         with pytest.raises(ValueError):
             Q.token_logprobs(*args)
+
+
+@pytest.mark.parametrize("work", [torch.zeros(1, dtype=torch.int8).expand(1 << 16), torch.zeros(1 << 17, dtype=torch.int8)[::2],
+                                  torch.zeros(1, 64).expand(1024, 64), torch.zeros(64, 1024).t()], ids=["one byte", "every other byte", "one row", "transposed"])
+def test_binding_refuses_workspaces_with_less_room_than_elements(work):
+    """A workspace that repeats its elements has fewer bytes than it counts; the gaps of one that skips some are another's."""
+    x, w, ws, y = torch.zeros(4, 32), torch.zeros(8, 32, dtype=torch.int8), torch.zeros(8), torch.zeros(4, 8)
+    with pytest.raises(ValueError, match="workspace"):
+        Q.linear_int8_dynamic(x, w, ws, None, y, work)
+    with pytest.raises(ValueError, match="workspace"):
+        Q.token_logprobs(torch.zeros(4, 100), entropy=torch.zeros(4), workspace=work)

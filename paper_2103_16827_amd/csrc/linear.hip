@@ -87,32 +87,35 @@ __device__ __forceinline__ int xcd_order(uint32_t unit, uint32_t n) {
 __device__ __forceinline__ uint32_t first_unit() { return (blockIdx.y << kGridShift) + blockIdx.x; }
 
 // The tile of this workgroup where every group's rows are cut into tiles of BM; false if there is none.  Rows are counted 64
-// groups at a time by a scan over the lanes; every wave does it for itself.
+// groups at a time by a scan over the lanes; every wave does it for itself.  Their tiles are unsigned numbers: offsets that fall
+// and rise again (which may give wrong values, never an access out of range) make up to 32 M / BM + 64 of them, 2^31 + 64.
 template <int BM>
 __device__ __forceinline__ bool group_tile(const LinearParams& L, const Order& o, uint32_t unit, int BN, Tile& t) {
   const int lane = threadIdx.x & 63;
   int a, b;                                 // the lane's group among the 64 from e0 on, and its tiles
-  auto upto = [&](int e0, int& n) __attribute__((always_inline)) {
+  auto upto = [&](int e0, uint32_t& n) __attribute__((always_inline)) {
     const int e = min(e0 + lane, L.E - 1);
     a = offset_at(L, e);
     b = offset_at(L, e + 1);
     n = e0 + lane < L.E && b > a ? (b - a + BM - 1) / BM : 0;
-    return wave_scan(n, 0, [](int x, int y) { return x + y; });
+    return wave_scan(n, 0u, [](uint32_t x, uint32_t y) { return x + y; });
   };
-  int n, before = upto(0, n), total = __builtin_amdgcn_readlane(before, 63);
-  for (int e0 = 64; e0 < L.E && total < o.mt; e0 += 64) total += __builtin_amdgcn_readlane(upto(e0, n), 63);
+  auto of_lane = [](uint32_t v, int from) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_readlane((int)v, from); };
+  const uint32_t most = o.mt;
+  uint32_t n, before = upto(0, n), total = of_lane(before, 63);
+  for (int e0 = 64; e0 < L.E && total < most; e0 += 64) total += of_lane(upto(e0, n), 63);
   if (L.E > 64) before = upto(0, n);
-  // (more than o.mt only where offsets decrease)
-  const int u = xcd_order(unit, (uint32_t)min(total, o.mt) * o.nt);
+  // (more than that only where offsets decrease)
+  const int u = xcd_order(unit, min(total, most) * o.nt);
   if (u < 0) return false;
-  int left = u / o.nt;
-  t.n0 = (u - left * o.nt) * BN;
+  uint32_t left = u / o.nt;
+  t.n0 = (u - (int)left * o.nt) * BN;
   for (int e0 = 0;;) {
-    const int all = __builtin_amdgcn_readlane(before, 63);
+    const uint32_t all = of_lane(before, 63);
     if (left < all) {
       const int src = __popcll(__ballot(before <= left));
       t.e = e0 + src;
-      t.lo = __builtin_amdgcn_readlane(a, src) + (left - __builtin_amdgcn_readlane(before - n, src)) * BM;
+      t.lo = __builtin_amdgcn_readlane(a, src) + (int)(left - of_lane(before - n, src)) * BM;
       t.hi = min(__builtin_amdgcn_readlane(b, src), t.lo + BM);
       return true;
     }

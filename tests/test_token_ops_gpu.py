@@ -638,3 +638,26 @@ def test_same_bits_every_time():
             s[k].fill_(1)
         for k, v in _run_chain(s).items():
             assert torch.equal(v, first[k]), k
+
+
+@pytest.mark.parametrize("rising", [True, False])
+def test_experts_of_as_many_rows_as_there_may_be(rising):
+    """2^30 rows in 96 groups; where the offsets fall and rise again, 48 groups of them: their tiles pass 2^31, the values are
+    undefined, and nothing outside y is written."""
+    print(f"[case] experts of 2^30 rows, rising offsets {rising}", flush=True)
+    g, M, E, N, K, T = gen(30), 1 << 30, 96, 2, 1024, 3
+    x, xs, w, ws = codes(g, T, K), scales(g, T), codes(g, E, N, K), scales(g, E, N)
+    offsets = torch.tensor([M // E * e + 5 * (e % 2) for e in range(E)] + [M] if rising else [M * (e % 2) for e in range(E + 1)]).int()
+    offsets[0] = 0
+    index = torch.arange(M, dtype=torch.int32, device="cuda").remainder_(T)
+    guard = 1 << 16
+    raw = torch.full((M * N + 2 * guard,), float(FILL), dtype=torch.bfloat16, device="cuda")
+    y = raw[guard:guard + M * N].view(M, N)
+    Q.experts_int8(x.cuda(), xs.cuda(), offsets.cuda(), index, w.cuda(), ws.cuda(), None, y)
+    torch.cuda.synchronize()
+    assert bool((raw[:guard] == FILL).all()) and bool((raw[guard + M * N:] == FILL).all())
+    if rising:
+        for e in range(E):
+            lo, hi = int(offsets[e]), int(offsets[e + 1])
+            want = linear_ref(x, xs, w[e], ws[e], None, torch.bfloat16).cuda()
+            assert bool((y[lo:hi] == want[index[lo:hi].long()]).all()), f"group {e}"

@@ -161,7 +161,7 @@ qasr_status qasr_experts_int8(const qasr_experts_desc* desc, const int8_t* x, co
 }
 
 static bool logprobs_shape_ok(int64_t rows, int32_t V, int32_t top) {
-  return rows >= 0 && rows <= ((int64_t)1 << 40) && V >= 1 && top >= 0 && top <= QASR_MAX_TOP && top <= V;
+  return rows >= 0 && rows <= ((int64_t)1 << 40) && V >= 1 && top >= 0 && top <= QASR_MAX_TOP && top <= V && rows_ok(rows, 0, V);
 }
 
 size_t qasr_logprobs_workspace_bytes(int64_t rows, int32_t V, int32_t top) {

@@ -182,3 +182,18 @@ def test_binding_refuses_workspaces_with_less_room_than_elements(work):
         Q.linear_int8_dynamic(x, w, ws, None, y, work)
     with pytest.raises(ValueError, match="workspace"):
         Q.token_logprobs(torch.zeros(4, 100), entropy=torch.zeros(4), workspace=work)
+
+
+@pytest.mark.parametrize("rows,V,top", [(1 << 40, (1 << 31) - 1, 64), (1 << 40, (1 << 18) + 1, 0), ((1 << 27) + 1, (1 << 31) - 1, 1), ((1 << 40) + 1, 1, 0)])
+def test_logprob_workspace_of_refused_sizes(rows, V, top):
+    """Logits whose addresses the call refuses have no workspace either (pieces of the first would pass 64 bits)."""
+    assert logprobs(x=f(1 << 50), rows=rows, V=V, top=top) == SHAPE
+    assert Q.logprobs_workspace_bytes(rows, V, top) == 0
+
+
+def test_logprob_workspace_of_the_most_logits():
+    """2^58 logits: pieces of at most 8 x 64 x 13 loads of 16 bytes, one of 12 bytes and `top` keys of 8 for each."""
+    rows, V, top = 1 << 27, (1 << 31) - 1, 64
+    pieces = -(-V * 4 // (8 * 64 * 13 * 16))
+    need = Q.logprobs_workspace_bytes(rows, V, top)
+    assert rows * pieces * (12 + 8 * top) <= need <= rows * 2 * pieces * (16 + 8 * top) + 256

@@ -465,7 +465,8 @@ qasr_status qasr_linear_int8(const qasr_linear_desc* d, const int8_t* x, const f
 /* qasr_quantize_tokens and qasr_linear_int8 in one call: x [M, K] of x_type, row stride d->x_stride; codes and scales live in the
  * workspace (device, 256-byte aligned, >= qasr_linear_workspace_bytes(M, K), else QASR_ERR_WORKSPACE; it must overlap none of the
  * tensors, and calls that may run at the same time need workspaces of their own).  The same bits as the two calls.  At most two kernels. */
-size_t qasr_linear_workspace_bytes(int32_t M, int32_t K);   /* HOST only; 0 on sizes that the call refuses */
+size_t qasr_linear_workspace_bytes(int32_t M, int32_t K);   /* HOST only; 0 if M <= 0, K < 1 or K > 131071 (the call's other
+                                                              * limits, M <= 2^30 among them, are the call's to refuse) */
 qasr_status qasr_linear_int8_dynamic(const qasr_linear_desc* d, const void* x, int32_t x_type, const int8_t* w,
                                      const float* w_scale, const float* bias, void* y, void* workspace,
                                      size_t workspace_bytes, void* stream);
@@ -501,7 +502,7 @@ qasr_status qasr_experts_int8(const qasr_experts_desc* d, const int8_t* x, const
  * is fine), else QASR_ERR_WORKSPACE; calls that may run at the same time need workspaces of their own.  Outputs and workspace must not
  * overlap x, tokens or each other.  At most two kernels. */
 #define QASR_MAX_TOP 64
-size_t qasr_logprobs_workspace_bytes(int64_t rows, int32_t V, int32_t top);   /* HOST only; 0 on sizes that the call refuses */
+size_t qasr_logprobs_workspace_bytes(int64_t rows, int32_t V, int32_t top);   /* HOST only; 0 on sizes that the call refuses with dense rows */
 qasr_status qasr_token_logprobs(const void* x, int32_t x_type, int64_t rows, int32_t V, int64_t x_stride, const int32_t* tokens,
                                 int32_t n, float* logprob, float* entropy, int32_t top, int32_t* top_ids, float* top_logprob,
                                 void* workspace, size_t workspace_bytes, void* stream);

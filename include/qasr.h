@@ -478,7 +478,8 @@ qasr_status qasr_linear_int8_dynamic(const qasr_linear_desc* d, const void* x, i
  * Groups may be empty; rows outside every group (before offsets[0], from offsets[E] on) are left as they were.  offsets should not
  * decrease: they are taken as min(max(offset, 0), M), a group that ends before it starts is empty, and where decreasing
  * offsets make groups share rows, or give the groups more rows than M together, the values of y are undefined (never an access out
- * of range).  A row whose index is outside [0, x_rows) counts as codes of zero.  Errors as above; E < 1, E > 4096,
+ * of range).  A row whose index is outside [0, x_rows) counts as codes of zero with a scale of 0 (where a bias is -0 the result is
+ * a zero of either sign).  Errors as above; E < 1, E > 4096,
  * (M/16 + E) (N/16 + 1) > 2^31 - 16, x_rows < 1 or an expert stride smaller than a matrix is QASR_ERR_SHAPE, and so is x_rows < M
  * without an index. */
 typedef struct {

@@ -168,7 +168,7 @@ __device__ __forceinline__ int row_of(int n) { return 4 * ((n / (4 * P)) & 3) + 
 template <typename T>
 constexpr int products_of(int NT) { return NT < 4 / (int)sizeof(T) ? NT : 4 / (int)sizeof(T); }
 
-// each operation rounds once, as the ABI says; the sum itself rounds where it passes 2^24.  No bias is -0: it changes nothing.
+// each operation rounds once, as the ABI says; the sum itself rounds where it passes 2^24.  No bias is an addition of 0.
 template <typename T>
 __device__ __forceinline__ T result(int acc, float sx, float ws, float bias) {
 #pragma clang fp contract(off)
@@ -185,7 +185,7 @@ __device__ __forceinline__ float channel_scale(const LinearParams& L, const Tile
   return L.w_scale[(int64_t)t.e * L.N + min(n, L.N - 1)];
 }
 __device__ __forceinline__ float channel_bias(const LinearParams& L, const Tile& t, int n) {
-  return L.bias ? L.bias[(int64_t)t.e * L.N + min(n, L.N - 1)] : -0.0f;
+  return L.bias ? L.bias[(int64_t)t.e * L.N + min(n, L.N - 1)] : 0.0f;
 }
 
 // ---- few tokens

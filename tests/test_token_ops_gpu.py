@@ -661,3 +661,36 @@ def test_experts_of_as_many_rows_as_there_may_be(rising):
             lo, hi = int(offsets[e]), int(offsets[e + 1])
             want = linear_ref(x, xs, w[e], ws[e], None, torch.bfloat16).cuda()
             assert bool((y[lo:hi] == want[index[lo:hi].long()]).all()), f"group {e}"
+
+
+def bits(t):
+    return t.cpu().contiguous().view(torch.int32 if t.dtype == torch.float32 else torch.int16)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(5, 40, 64), (40, 200, 512), (300, 520, 400), (5, 40, 67), (300, 520, 401)])
+def test_linear_zeros_have_the_definitions_sign(M, N, K, dtype):
+    """Products that are zeros of either sign: without a bias 0 is added to them, a bias of -0 leaves them as they are."""
+    print(f"[case] linear zeros {M} x {N} x {K} {dtype}", flush=True)
+    g = gen(M + N + K)
+    x, w, xs, ws = codes(g, M, K), codes(g, N, K), scales(g, M), scales(g, N)
+    x[1] = 0
+    w[::3] = 0
+    xs[::2] *= -1
+    ws[::2] *= -1
+    xs[2] = 0.0
+    xs[3] = -0.0
+    ws[5] = 0.0
+    for bias in (None, torch.zeros(N), -torch.zeros(N)):
+        y = torch.empty(M, N, dtype=dtype, device="cuda")
+        Q.linear_int8(x.cuda(), xs.cuda(), w.cuda(), ws.cuda(), None if bias is None else bias.cuda(), y)
+        want = linear_ref(x, xs, w, ws, torch.zeros(N) if bias is None else bias, dtype)
+        assert torch.equal(bits(y), bits(want)), "no bias" if bias is None else f"bias {float(bias[0])}"
+    index = torch.arange(M, dtype=torch.int32)
+    index[::2] = torch.tensor([-1, M, 1 << 30]).int()[torch.arange((M + 1) // 2) % 3]
+    there = (index >= 0) & (index < M)
+    want = linear_ref(x * there[:, None], xs * there, w, ws, torch.zeros(N), dtype)
+    y = torch.empty(M, N, dtype=dtype, device="cuda")
+    Q.experts_int8(x.cuda(), xs.cuda(), torch.tensor([0, M // 3, M]).int().cuda(), index.cuda(), torch.stack([w, w]).cuda(),
+                   torch.stack([ws, ws]).cuda(), None, y)
+    assert torch.equal(bits(y), bits(want)), "experts"

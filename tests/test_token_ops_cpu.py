@@ -197,3 +197,21 @@ def test_logprob_workspace_of_the_most_logits():
     pieces = -(-V * 4 // (8 * 64 * 13 * 16))
     need = Q.logprobs_workspace_bytes(rows, V, top)
     assert rows * pieces * (12 + 8 * top) <= need <= rows * 2 * pieces * (16 + 8 * top) + 256
+
+
+def test_binding_refuses_what_is_no_matrix():
+    """A tensor of too few or too many dimensions is a ValueError as well, in every place."""
+    i8, i32, f32 = (lambda *s, d=d: torch.zeros(*s, dtype=d) for d in (torch.int8, torch.int32, torch.float32))
+    x, xs, w, ws, y = i8(4, 32), f32(4), i8(8, 32), f32(8), f32(4, 8)
+    off, idx, we, wse, work, lg = i32(4), i32(4), i8(3, 8, 32), f32(3, 8), i8(512), f32(4, 100)
+    for call, args in [(Q.quantize_tokens, (f32(4), i8(4), xs)), (Q.quantize_tokens, (f32(()), i8(()), xs)), (Q.linear_int8, (i8(()), xs, w, ws, None, y)),
+                       (Q.linear_int8, (x, xs, i8(()), ws, None, y)), (Q.linear_int8, (x, xs, i8(8), ws, None, y)), (Q.linear_int8, (x, xs, w, ws, None, f32(()))),
+                       (Q.linear_int8_dynamic, (f32(4, 32), i8(()), ws, None, y, work)), (Q.linear_int8_dynamic, (f32(4, 32), i8(8, 32, 1), ws, None, y, work)),
+                       (Q.experts_int8, (x, xs, off, idx, we, wse, None, f32(()))), (Q.experts_int8, (x, xs, off, idx, we, wse, None, f32(4))),
+                       (Q.experts_int8, (x, xs, off, i32(()), we, wse, None, y)), (Q.experts_int8, (x, xs, off, i32(4, 1), we, wse, None, y)),
+                       (Q.experts_int8, (x, xs, off, idx, i8(3), wse, None, y)), (Q.experts_int8, (x, xs, off, idx, i8(3, 8, 32, 1), wse, None, y)),
+                       (Q.token_logprobs, (lg, i32(4), f32(4))), (Q.token_logprobs, (lg, i32(()), f32(()))), (Q.token_logprobs, (lg, i32(4, 1, 1), f32(4, 1, 1))),
+                       (Q.token_logprobs, (lg, None, None, None, i32(4), f32(4))), (Q.token_logprobs, (lg, None, None, None, i32(()), f32(()))),
+                       (Q.token_logprobs, (f32(100), None, None, f32(1)))]:
+        with pytest.raises(ValueError):
+            call(*args)

@@ -24,6 +24,7 @@
 #include "lanes.hpp"
 #include "launch_shape.hpp"
 #include "quantize_row.hpp"
+#include "tuning.hpp"
 #include "vmem.hpp"
 
 #include <algorithm>
@@ -762,6 +763,7 @@ double groups_of(const LinearParams& p) { return p.offsets ? p.E * (1.0 - std::p
 // and lose more where the cache does (17.4 for 13.2).
 constexpr int64_t kLargeWeights = 1 << 28;
 bool weights_once(const LinearParams& p, int BM) {
+  if (const int forced = tuning().linear_once) return forced == 2;
   return (int64_t)(p.offsets ? p.E : 1) * p.N * p.K >= kLargeWeights && p.M <= (p.offsets ? 1 : 2) * BM * groups_of(p);
 }
 
@@ -847,6 +849,7 @@ constexpr double kBytesPerUs = 5.3e6;           // of memory
 
 template <int N>
 int fastest_form(const LinearParams& p, const Form (&forms)[N], int among) {
+  if (const int forced = tuning().linear_form; forced >= 1 && forced <= among) return forced - 1;
   const double steps = (p.K + 127) / 128, units = compute_units();
   const double groups = groups_of(p), rows = p.M / groups;
   const double memory = (groups * p.N * p.K + (double)p.M * (p.K + 2.0 * p.N)) / kBytesPerUs;

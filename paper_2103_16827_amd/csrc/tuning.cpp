@@ -57,6 +57,10 @@ Tuning read_env() {
     int mt = 0, nt = 0, ks = 0;
     if (sscanf(e, "%d,%d,%d", &mt, &nt, &ks) >= 1) { t.sep_mt = mt; t.sep_nt = nt; t.sep_ks = ks; }
   }
+  if (const char* e = getenv("QASR_LINEAR")) {
+    int f = 0, w = 0;
+    if (sscanf(e, "%d,%d", &f, &w) >= 1) { t.linear_form = f; t.linear_once = w; }
+  }
   if (const char* e = getenv("QASR_PWT_MT")) t.pwt_mt = atoi(e);
   if (const char* e = getenv("QASR_SLOT_DEPTH")) {
     const int d = atoi(e);

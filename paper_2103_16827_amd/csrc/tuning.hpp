@@ -24,6 +24,9 @@
 //   QASR_NO_SEP                             encoder: no depthwise + pointwise pair in one launch
 //   QASR_SEP = "MT,NT[,KS]"                 the same: groups per tile, 16-channel columns per wave (0: free), wave groups over
 //                                           the input channels (1 where NT is given alone)
+//   QASR_LINEAR = "F[,W]"                   linear layers, experts: form F of linear.hip's table for the rows' alignment, from 1 on (0, or
+//                                           one that there is not: the model's choice), weights past the cache never (W = 1) or
+//                                           always (2; 0: by their size)
 //   QASR_TEAM                               encoder: plan runs of layers for the persistent team kernel
 //                                           (experimental, off unless set)
 #pragma once
@@ -40,6 +43,7 @@ struct Tuning {
   int sep_mt = 0, sep_nt = 0, sep_ks = 0, pww_mt = 0, pww_ks = 0, chain_mt = 0;
   int slot_depth = 4;
   int cf_nt = 0;
+  int linear_form = 0, linear_once = 0;
 };
 
 const Tuning& tuning();

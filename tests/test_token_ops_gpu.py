@@ -694,3 +694,25 @@ def test_linear_zeros_have_the_definitions_sign(M, N, K, dtype):
     Q.experts_int8(x.cuda(), xs.cuda(), torch.tensor([0, M // 3, M]).int().cuda(), index.cuda(), torch.stack([w, w]).cuda(),
                    torch.stack([ws, ws]).cuda(), None, y)
     assert torch.equal(bits(y), bits(want)), "experts"
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,K", [(2050, 300), (2049, 1000), (2300, 2047), (600, 2500), (513, 4095), (520, 8190), (2048, 5), (515, 16383)])
+def test_quantize_tokens_many_rows(M, K, dtype):
+    """So many rows that a wave, or four, take what more of them take where there are few; rows of zeros, infinities and NaN among them."""
+    print(f"[case] quantize {M} x {K} {dtype}", flush=True)
+    g = gen(M * 31 + K)
+    x = (torch.randn(M, K, generator=g) * torch.rand(M, 1, generator=g) * 10).to(dtype)
+    x[1] = 0.0
+    x[2, K // 2] = float("inf")
+    x[3, 0], x[3, K - 1] = float("-inf"), float("nan")
+    x[4] = float("nan")
+    x[5] = float("-inf")
+    x[M - 1, K - 1] = float("inf")
+    for pad, qpad, shift in ((0, 0, 0), (5, 3, 1)):
+        xp, qp, scale = Padded(M, K, dtype, K + pad, shift, x), Padded(M, K, torch.int8, K + qpad, shift), torch.empty(M, device="cuda")
+        Q.quantize_tokens(xp.view, qp.view, scale)
+        q, S = quantize_ref(x)
+        same(scale, S, "scales")
+        same(qp.view, q, "codes")
+        qp.check()

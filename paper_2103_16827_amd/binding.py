@@ -439,7 +439,7 @@ def _room(t):
         return 0
     if not t.is_contiguous():
         _refuse("workspace", t, "a dense tensor")
-    return t.numel() * t.element_size()
+    return t.nbytes
 
 
 def quantize_tokens(x, q, scale):
@@ -463,7 +463,7 @@ def _linear_desc(M, N, K, xs, w, w_scale, bias, y):
 
 def linear_int8(x, x_scale, w, w_scale, bias, y):
     """qasr_linear_int8: codes x [M, K] and w [N, K] with scales [M] and [N] (and bias [N] or None) -> float y [M, N]."""
-    (M, K), (N, *_) = x.shape, w.shape
+    (M, K), (N, _) = x.shape, w.shape
     d = _linear_desc(M, N, K, _codes(x, (M, K), "x"), w, w_scale, bias, y)
     _dense(x_scale, _f32, (M,), "x_scale")
     stream = _on_device(x, x_scale, w, w_scale, bias, y)
@@ -478,7 +478,7 @@ def linear_workspace_bytes(M: int, K: int) -> int:
 
 def linear_int8_dynamic(x, w, w_scale, bias, y, workspace):
     """qasr_linear_int8_dynamic: float x [M, K], quantised token by token in the workspace, through codes w [N, K] -> float y."""
-    (M, K), (N, *_) = x.shape, w.shape
+    (M, K), (N, _) = x.shape, w.shape
     kind = _float_type(x, "x")
     d, room = _linear_desc(M, N, K, _rows(x, (M, K), "x"), w, w_scale, bias, y), _room(workspace)
     stream = _on_device(x, w, w_scale, bias, y, workspace)
@@ -490,13 +490,13 @@ def linear_int8_dynamic(x, w, w_scale, bias, y, workspace):
 def experts_int8(x, x_scale, offsets, index, w, w_scale, bias, y):
     """qasr_experts_int8: rows offsets[e] .. offsets[e + 1] of y [M, N] through w[e] of codes w [E, N, K]; row r reads row
     index[r] of the codes x [x_rows, K] (row r without an index).  Rows of y that the index has no entry for stay as they are."""
-    (rows, K), (E, N, *_), (M, *_), out = x.shape, w.shape, y.shape, y
+    (rows, K), (E, N, _), (M, _), out = x.shape, w.shape, y.shape, y
     if index is not None:
-        indexed, *_ = index.shape
+        indexed, = index.shape
         if indexed < M:
             M, y = indexed, y[:indexed]
     xs, st = _codes(x, (rows, K), "x"), w.stride()
-    if w.dim() != 3 or w.dtype is not _int8 or w.shape[2] != K or (st[2] != 1 and K > 1) or \
+    if w.dtype is not _int8 or w.shape[2] != K or (st[2] != 1 and K > 1) or \
             (st[1] < K and N > 1) or (st[0] < st[1] * (N - 1) + K and E > 1):
         _refuse("w", w, f"int8 of ({E}, {N}, {K}) with contiguous rows that do not overlap")
     _dense(x_scale, _f32, (rows,), "x_scale")
@@ -523,8 +523,8 @@ def token_logprobs(x, tokens=None, logprob=None, entropy=None, top_ids=None, top
     entropy [rows], and the top alternatives' ids and log probabilities [rows, top].  What is not asked for is None."""
     rows, V = x.shape
     kind, xs = _float_type(x, "x"), _rows(x, (rows, V), "x")
-    *_, n = tokens.shape if tokens is not None else (0,)
-    *_, top = top_ids.shape if top_ids is not None else (0,)
+    _, n = tokens.shape if tokens is not None else (rows, 0)
+    _, top = top_ids.shape if top_ids is not None else (rows, 0)
     if tokens is not None or logprob is not None:
         if tokens is None or logprob is None:
             raise ValueError("tokens and logprob go together")

@@ -430,7 +430,8 @@ int32_t qasr_probe_mfma_i8_outputs(void);
 qasr_status qasr_probe_mfma_i8(int32_t iters, int32_t* out, double* ops, void* stream);
 
 /* ---- Language-model operators: what scores or produces a transcript next to the encoders.  Token-major tensors
- * (one row per token), int8 codes with a scale per token and per channel, float results.  Inference only, like everything here.
+ * (one row per token: an encoder's [B, C, T] has to be transposed by the caller first), int8 codes with a scale per token and per
+ * channel, float results.  Inference only, like everything here.
  *
  * Element types of float tensors.  Float pointers must be aligned to their element (else QASR_ERR_PARAM); rows may start anywhere
  * else and be any distance apart (strides in elements, 0 => dense rows).  Unless a call says otherwise it enqueues one kernel. */

@@ -10,14 +10,15 @@
 // linear_few (few tokens): the weights pass once from memory to one workgroup, which is all such a product costs.  The waves
 // of a workgroup split K, each with a ring of its own in LDS and no barrier before the end, where the exact int32
 // partial sums meet in LDS.  Bound by memory, and below 16 MB of weights by one launch and its chain of loads: 1 token of 4096 x 4096
-// 5.4 us, 32 of 11008 x 4096 10.7 with the weights in the 256 MB cache, 15.6 from memory (2.9 TB/s), 1 of 32768 x 4096 21 (6.3 TB/s).
-// linear_tile (more): tiles of BM x BN through a ring in LDS that the waves share, a barrier per step.  8192 x 14336 x 4096 355 us =
-// 2.7 POP/s, 8192^3 384 = 2.9: matrix pipes 62 % busy at the 1.9 GHz that the operands' power leaves (zeros instead of codes: 9 %
-// faster).  A step of a 256 x 256 tile keeps the LDS port (192 KiB read, 64 written, 128 bytes a cycle) as long as the products keep the
+// 4.9 us with the weights in the 256 MB cache and 6.8 from memory, 32 of 11008 x 4096 10.6 and 15.3 (3.0 TB/s), 1 of 32768 x 4096 29.8 from
+// memory (4.5 TB/s).
+// linear_tile (more): tiles of BM x BN through a ring in LDS that the waves share, a barrier per step.  8192 x 14336 x 4096 372 to 400 us by
+// the card = 2.4 to 2.6 POP/s, 8192^3 384 to 438 = 2.5 to 2.9: matrix pipes 62 % busy at the 1.9 GHz that the operands' power leaves (zeros instead of
+// codes, on a card that takes 400 us: 300).  A step of a 256 x 256 tile keeps the LDS port (192 KiB read, 64 written, 128 bytes a cycle) as long as the products keep the
 // pipes.  Four waves of 128 x 128 each instead of eight of 128 x 64, which read a third less, have one wave per SIMD and were 3 to 6 % slower;
 // stages of 64 codes, three of them, too, at half the vector cache's rate; tiles in turn with the results of one leaving under the
 // products of the next spilled registers.
-// linear_rows: the same tiles for rows of any alignment, through registers.  777 x 1029 x 1003 7.8 us, 2000 x 2001 x 2001 24.5
+// linear_rows: the same tiles for rows of any alignment, through registers.  777 x 1029 x 1003 7.6 to 8.0 us, 2000 x 2001 x 2001 24.4
 // (0.66 POP/s): its chain of loads, two steps ahead.
 #include "floats.hpp"
 #include "kernels.hpp"
@@ -466,9 +467,10 @@ struct Scales {
 // so that they leave as whole cache lines: from the registers, where a lane has 16 bytes of every product or two, they would go
 // as 64-byte pieces.  Piece p of a row is at p ^ (row & 7).
 // Rows that keep to boundaries of 64 bytes are stored past the caches, so that no workgroup leaves a 4 MB L2 full of lines to
-// be written out, and the operands stay there: 8192 x 14336 x 4096 364 us for 402, 4096 x 4096 x 512 15.5 for 17.9, and with the
-// layer that quantises the result behind it no slower (6400 x 2048 x 512: 38.6 us for 44.8 together).  Lines that two workgroups
-// share have to meet in the cache: 4096 x 4104 x 512 took 30.4 us past it, 27.8 through it.
+// be written out, and the operands stay there: 8192 x 14336 x 4096 401 us for 408 on one card (364 for 402 on another), 4096 x 4096 x 512 15.5
+// for 16.1, and no difference for 6400 x 2048 x 512 in float32 (17.7 and 17.9), alone or with the layer that quantises the result behind it
+// (44.1 and 43.8 together).  Lines that two workgroups share have to meet in the cache: 4096 x 4104 x 512 took 30.4 us past it, 25 to 28
+// through it.
 template <int MT, int NT, int BM, int BN, int ROOM, typename T>
 __device__ __forceinline__ void store_tile(const LinearParams& L, const Tile& t, const float* scales, unsigned char* room, int m0, int n0,
                                            const Sums<MT, NT>& acc) {
@@ -758,9 +760,9 @@ double groups_of(const LinearParams& p) { return p.offsets ? p.E * (1.0 - std::p
 
 // ONCE: the weights come past the 256 MB cache behind the L2s.  That is for matrices, all experts' together, that are larger than
 // the cache, and for as many rows as a tile has, of one matrix as two tiles that run side by side: 64 experts of 2048 x 2048 with
-// 8 rows each 44.3 us for 50.6, with 32 rows 50.1 for 54.9, 128 of 1024 x 2048 with a row each 27.4 for 29.3.  With two tiles to most of
-// 64 experts of 2816 x 2048 it is 165 us for 152.  Smaller matrices gain less where memory has them (32 x 11008 x 4096 14.9 us for 15.6),
-// and lose more where the cache does (17.4 for 13.2).
+// 8 rows each 45.2 us for 52.6, with 32 rows 44.9 for 50.5, 128 of 1024 x 2048 with a row each 28.6 for 32.9.  With two tiles to most of
+// 64 experts of 2816 x 2048 it is one or the other by the card (163 us for 167, 165 for 152).  Smaller matrices gain less where memory has
+// them (32 x 11008 x 4096 14.8 us for 15.2), and lose more where the cache does (12.9 for 10.6).
 constexpr int64_t kLargeWeights = 1 << 28;
 bool weights_once(const LinearParams& p, int BM) {
   if (const int forced = tuning().linear_once) return forced == 2;
@@ -819,8 +821,9 @@ bool direct_ok(const LinearParams& p) {
 
 // What a form of the kernels takes for one tile on a compute unit, in us: `end` for its beginning and end, `group` more of that
 // where a tile's rows have to be found first, and for a step of 128 codes `alone` with nothing else on the chip, `busy` with
-// a tile on every unit.  Fitted to 10 forms x 36 shapes of 1 to 16384 rows, 10 of them in groups, on weights that no cache held (rms 6 to 16 %
-// by form); next to the fastest form of each shape, the one that the rule takes cost nothing in 32 of them and at most 9 %.
+// a tile on every unit.  Fitted to 10 forms x 36 shapes of 1 to 16384 rows, 10 of them in groups, on weights that no cache held; against the
+// same shapes timed anew, its times are off by 9 to 20 % rms by form, and the form that it takes is within 1 % of the fastest for 27 of them, within 10 %
+// for 34, and 16 % and 31 % slower for 64 and 256 rows of 4096 x 4096 (2.4 % on average; profiles/linear_form_choice.txt has them all).
 struct Form { int BM, BN, per_unit; double end, group, alone, busy; };
 constexpr Form kForms[] = {
     {16, 16, 5, 0.29, 1.5, 0.085, 0.039},      // linear_few, from here
@@ -834,8 +837,8 @@ constexpr Form kForms[] = {
     {128, 256, 1, 3.39, 0.48, 0.556, 0.907},
     {256, 256, 1, 3.11, 1.71, 1.216, 1.216},
 };
-// ... where rows begin anywhere or end inside a chunk (20 shapes: rms 7 to 12 %, the rule takes the fastest form or one within 2 % for 16 of
-// them, within 6 % for three more and 12 % for the last)
+// ... where rows begin anywhere or end inside a chunk (20 shapes: off by 11 to 13 % rms, the form within 1 % of the fastest for 14 of them, within 7 %
+// for five more and 10 % slower for the last)
 constexpr Form kRowForms[] = {
     {16, 16, 4, 0.65, 1.43, 0.116, 0.087},     // linear_few, 8 waves
     {16, 32, 6, 0.31, 1.33, 0.204, 0.142},     // 4 waves
@@ -899,7 +902,8 @@ hipError_t launch_typed(const LinearParams& p, hipStream_t st) {
 }  // namespace
 
 // Few enough floats for every workgroup to quantise them: with kFloats over all rounds of workgroups on the chip it takes
-// less than the launch that it saves (one token of 2048 x 2048: 6.7 us a call, 10.0 as two kernels).
+// less than the launch that it saves (one token of 2048 x 2048 in a graph: 4.2 us, 5.7 as two kernels; called from the host 6.7, and 12.2
+// as two calls).
 bool linear_takes_floats(const LinearParams& p, int x_type) {
   const int64_t size = x_type == 0 ? 4 : 2, all = (int64_t)p.M * p.K;
   LinearParams codes = p;                // as if tokens were codes on a boundary: the weights are what is asked about

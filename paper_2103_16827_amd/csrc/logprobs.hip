@@ -14,9 +14,11 @@
 // Pieces leave (m, s, t) and their best in the workspace; a second kernel joins them.
 // What bounds it: the logits' way from memory, and next to it about eleven vector operations per logit, of which the
 // exponential takes four times the others' time.  4096 rows of 50257 bf16 logits 73 us (5.6 TB/s), with 5 alternatives 79, with 20 81;
-// 64 of 151936 fp16 11.3 and 15.0; 1 of 128256 float32 5.4 and 10.4, of which a launch and its first loads are half, the second
-// kernel another half.  With 3 logits left of 50257 and 20 alternatives, 512 rows take 42 us for 19 (657 when they were taken out one
-// after the other).
+// 64 of 151936 fp16 11.3 and with 20 alternatives 15.1 (12.3 and 16.0 from memory); 1 of 128256 float32 5.4 and 10.3, of which a launch and its
+// first loads are half, the second kernel another half.  With 3 logits left of 50257 and 20 alternatives, 512 rows take 43 us for 20 (657 when they
+// were taken out one after the other).
+// The exponential and the logarithm are the hardware's (__expf, __logf: an ulp of their own, and of an exponential's argument d another 2^-24 |d|): an
+// exponential that matters has a small |d|, and a sum's rounding is of the same size.
 #include "floats.hpp"
 #include "kernels.hpp"
 #include "lanes.hpp"
@@ -632,10 +634,12 @@ int size_of(int type) { return type == 0 ? 4 : 2; }
 constexpr int kWhole = 16 * 64 * 8 * 16, kPiece = 8 * 64 * 13 * 16;
 
 // A row that one workgroup can take is one piece: it is done before a second kernel would begin (32000 float32 logits and five
-// alternatives 6.7 us, 9.9 in 15 pieces; 1000 such rows 26.5, 33.4 in two).  Few long rows: pieces for the whole chip, of 8 KiB and
+// alternatives 6.6 us, 8.4 in two pieces, 9.9 in 15; 256 such rows 10.9 and 13.9 in two; but 1000 of them 39.5 and 31.0: 16 waves of 8 loads
+// have a unit to themselves, of 8 waves two share it).  Few long rows: pieces for the whole chip, of 8 KiB and
 // more, whose best the workgroup that joins them can hold.  Else the number of them that leaves the busiest compute unit the least
-// to do, up to twice as many as it takes (128 rows of 128256 fp16 logits with 20 alternatives 20.1 us in 4 pieces, 20.9 in 2, 22.4 in
-// 3; 1000 of 100000 49.4 in 2, 52.4 in 3, 54.7 in 4).
+// to do, up to twice as many as it takes (128 rows of 128256 fp16 logits with 20 alternatives 18.7 to 20.1 us in 4 pieces, 20.9 in 2, 22.4
+// in 3; 1000 of 100000 49.4 in 2, 52.4 in 3, 54.7 in 4).  256: the chip's units, as a number, because the workspace's size has to be the same
+// whichever device is current, or none.
 Pieces pieces_of(int64_t rows, int V, int bytes, int top) {
   Pieces c{};
   const int64_t all = (int64_t)V * bytes;
@@ -682,8 +686,9 @@ hipError_t launch_logprobs(const LogprobParams& p, int x_type, void* workspace, 
       const GridShape g = grid_shape(waves == 1 ? (units + 3) / 4 : units);
       return launch_kernel(kernel, dim3(g.x, g.y), dim3(waves == 1 ? 256 : 64 * waves), 0, st, p, c);
     };
-    // (25600 rows of 128 float32 logits and 5 alternatives 9.2 us, a wave a row 21.7, 16 rows 3.7 and 4.7; 25600 of 256 bf16 and 8 alternatives
-    // 17.9 and 24.6, but 1000 rows 6.6 and 5.4)
+    // (25600 rows of 128 float32 logits and 5 alternatives 9.4 us, a wave a row 22.6, 16 rows 3.7 and 4.7; 25600 of 256 bf16 and 8 alternatives
+    // 19.8 and 25.2, but 1000 rows 6.6 and 5.4; with more alternatives a wave a row is the faster one for 256 logits, 28.6 for 33.3 with 20,
+    // not for 128, 25.2 for 20.4)
     if (p.V <= 64 || (p.V <= 128 && p.top <= 5) || (p.V <= 256 && p.top <= 8 && p.rows >= 4096)) {
       const int G = p.V <= 16 ? 4 : p.V <= 32 ? 8 : 16, rows = 4 * 64 / G;
       const GridShape g = grid_shape((p.rows + rows - 1) / rows);
@@ -692,8 +697,8 @@ hipError_t launch_logprobs(const LogprobParams& p, int x_type, void* workspace, 
                            dim3(g.x, g.y), dim3(256), 0, st, p);
     }
     // As many registers as a row needs and as few waves as then hold it: rows meet fewer barriers, and more of them share a unit.
-    // (4096 rows of 50257 bf16 logits and 20 alternatives: 8 waves of 13 loads 82 us, 16 of 8 99; of 18000: 4 of 10 37 us, 8 of 8 48, but
-    // where there are few rows, 16 of 20000, 7.6 us against 6.9)
+    // (4096 rows of 50257 bf16 logits and 20 alternatives: 8 waves of 13 loads 81 us, 16 of 8 168; of 18000: 4 of 10 37 us, 8 of 8 48, but
+    // where there are few rows, 16 of 20000, 7.8 us against 6.9; profiles/logprobs_form_choice.txt has every kernel beside the choice)
     if (loads <= 64) e = launch(logprobs_kernel<T, 1, 1>, 1);
     else if (loads <= 256) e = launch(logprobs_kernel<T, 1, 4>, 1);
     else if (loads <= 512) e = launch(logprobs_kernel<T, 4, 2>, 4);

@@ -4,7 +4,7 @@
 // (as unsigned numbers, whose order is that of floats: two 16-bit ones at a time), then a correctly rounded division, a
 // rounding and a conversion per element.  What bounds it is memory (3 to 5 bytes an element); the division's eleven
 // instructions stay below that.  Rows longer than the registers are read twice.
-// 8192 x 8192: bf16 41.6 us (4.8 TB/s), float32 60.5 (5.5); 16384 x 512 bf16 8.4; one token of 4096 2.4, most of it the launch.
+// 8192 x 8192: bf16 41.5 us (4.8 TB/s), float32 60.6 (5.5); 16384 x 512 bf16 7.8; one token of 4096 2.4, most of it the launch.
 // Codes stored past the caches would save 2 to 15 % here, and cost the layer that reads them next more (2000 x 2048 into 512
 // channels: 22.9 us for both against 21.1).
 #include "floats.hpp"

@@ -821,7 +821,7 @@ bool direct_ok(const LinearParams& p) {
 
 // What a form of the kernels takes for one tile on a compute unit, in us: `end` for its beginning and end, `group` more of that
 // where a tile's rows have to be found first, and for a step of 128 codes `alone` with nothing else on the chip, `busy` with
-// a tile on every unit.  Fitted to 10 forms x 36 shapes of 1 to 16384 rows, 10 of them in groups, on weights that no cache held; against the
+// a tile on every unit.  Fitted to 10 forms x 36 shapes of 1 to 16384 rows, 10 of them in groups, on several copies of the weights in turn; against the
 // same shapes timed anew, its times are off by 9 to 20 % rms by form, and the form that it takes is within 1 % of the fastest for 27 of them, within 10 %
 // for 34, and 16 % and 31 % slower for 64 and 256 rows of 4096 x 4096 (2.4 % on average; profiles/linear_form_choice.txt has them all).
 struct Form { int BM, BN, per_unit; double end, group, alone, busy; };
